@@ -1,0 +1,547 @@
+"""The operators that a block of a language model adds to libmesa, as cases that can be prepared, run and timed.
+
+A case is a dict of plain values; `op` says which operator it runs:
+
+  bounds     the interval of keys that each query sees, from lengths, a causal order, a window, prefixes and documents
+  rope       the forward of a packed query/key/value projection: the norm of each query and key head, the rotation by
+             position (one axis or several), the 8-bit codes of everything, the running estimates
+  rope_bwd   its backward: queries and keys again from the codes, then the gradients of the projection and of the gains
+  attend     attention over intervals of keys, with capped scores and a bias by distance: output and log-sum-exp
+  attend_bwd its backward at operands that were saved as 8-bit codes or made again from them
+
+`own` false: elementary torch operations, in 32 bits or more; `own` true: the calls of the library. `exact` gives the same
+outputs in 64 bits. Sizes are those of this repository's configurations (197 tokens, 12 heads of 64; 8 x 4096 tokens, 16 heads
+of 64) and generic ones (heads of 128 that share keys and values, packed documents, long caches).
+"""
+from __future__ import annotations
+
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False
+DEV = "cuda:0"
+DTYPES = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+LAM = 0.9
+EPS = 1e-6
+if torch.cuda.is_available():
+    torch.backends.cuda.matmul.allow_tf32 = False
+
+
+# ---------------------------------------------------------------------------------------------------------------- cases
+def listed():
+    return [
+        # the mask of a padded batch of sequences, causal with a window: a short call once per training step
+        dict(name="bounds_padded_batch", op="bounds", B=8, Nq=4096, Nk=4096, causal=True, window=1024, docs=0, prefix=False, pad=True),
+        # long packed rows of documents, each with a prefix that all of its tokens see
+        dict(name="bounds_packed_documents", op="bounds", B=64, Nq=32768, Nk=32768, causal=True, window=0, docs=61, prefix=True, pad=True),
+        # one new token of one sequence: latency
+        dict(name="rope_one_token_f16", op="rope", dtype="f16", T=1, Hq=16, Hk=4, Hv=4, D=64, rot=64, axes=1, interleaved=False, norm=True),
+        # a training step's 8 x 4096 tokens, heads of 128 with four queries to a key
+        dict(name="rope_32k_tokens_bf16", op="rope", dtype="bf16", T=32768, Hq=32, Hk=8, Hv=8, D=128, rot=128, axes=1, interleaved=False, norm=True),
+        # image tokens with three position axes, binary32, odd count (7 images of 197 tokens), rotation of half a head
+        dict(name="rope_bwd_image_f32", op="rope_bwd", dtype="f32", T=1379, Hq=6, Hk=6, Hv=6, D=64, rot=32, axes=3, interleaved=True, norm=True),
+        # the backward of the training step above
+        dict(name="rope_bwd_32k_tokens_bf16", op="rope_bwd", dtype="bf16", T=32768, Hq=32, Hk=8, Hv=8, D=128, rot=128, axes=1, interleaved=False, norm=True),
+        # one new token of each of 16 sequences over long caches of different lengths, eight queries to a key
+        dict(name="attend_one_token_bf16", op="attend", dtype="bf16", B=16, Nq=1, Nk=16381, Hq=32, Hk=4, D=128, causal=True, window=0, docs=0, prefix=False, pad=True,
+             cap=0.0, bias=False),
+        # the long-sequence block of this repository's configurations: 8 x 4096 tokens, 16 heads of 64, causal
+        dict(name="attend_4096_f16", op="attend", dtype="f16", B=8, Nq=4096, Nk=4096, Hq=16, Hk=16, D=64, causal=True, window=0, docs=0, prefix=False, pad=False,
+             cap=0.0, bias=False),
+        # long sequences with capped scores, heads of 128 that share keys
+        dict(name="attend_8192_cap_bf16", op="attend", dtype="bf16", B=2, Nq=8192, Nk=8192, Hq=16, Hk=4, D=128, causal=True, window=0, docs=0, prefix=False, pad=False,
+             cap=30.0, bias=False),
+        # the attention of an image block: 12 heads, 197 tokens, everything seen, all three operands saved as codes
+        dict(name="attend_bwd_197_codes_f16", op="attend_bwd", dtype="f16", B=32, Nq=197, Nk=197, Hq=12, Hk=12, D=64, causal=False, window=0, docs=0, prefix=False,
+             pad=False, cap=0.0, bias=False, codes="qkv"),
+        # packed documents with a bias by distance
+        dict(name="attend_bwd_documents_f16", op="attend_bwd", dtype="f16", B=4, Nq=4001, Nk=4001, Hq=16, Hk=4, D=64, causal=True, window=0, docs=5, prefix=False,
+             pad=True, cap=0.0, bias=True, codes="v"),
+        # a training step's long sequences, heads of 128 that share keys
+        dict(name="attend_bwd_4096_bf16", op="attend_bwd", dtype="bf16", B=4, Nq=4096, Nk=4096, Hq=16, Hk=4, D=128, causal=True, window=0, docs=0, prefix=False,
+             pad=False, cap=0.0, bias=False, codes="v"),
+    ]
+
+
+def _log(rng, low, high):
+    return int(round(math.exp(rng.uniform(math.log(low), math.log(high)))))
+
+
+def draw(rng):
+    op = rng.choice(["bounds", "rope", "rope_bwd", "attend", "attend", "attend_bwd", "attend_bwd"])
+    mask = dict(causal=rng.random() < 0.8, window=rng.choice([0, 0, _log(rng, 16, 2048)]), docs=rng.choice([0, 0, rng.randint(1, 40)]), prefix=rng.random() < 0.25,
+                pad=rng.random() < 0.5)
+    if op == "bounds":
+        Nq = _log(rng, 1, 28000)
+        return dict(op=op, B=_log(rng, 1, 64), Nq=Nq, Nk=Nq + rng.choice([0, _log(rng, 1, 4096)]), **mask)
+    if op in ("rope", "rope_bwd"):
+        dtype = rng.choice(["f16", "bf16", "bf16", "f32"])
+        T = _log(rng, 1, 15000 if dtype == "f32" else 30000)
+        D = rng.choice([32, 64, 80, 96, 128, 256])
+        Hk = rng.choice([1, 2, 3, 4, 8])
+        Hq = Hk * rng.choice([1, 2, 4])
+        while (Hq + 2 * Hk) * D > 6144:
+            Hq, Hk = max(1, Hq // 2), max(1, Hk // 2)
+        return dict(op=op, dtype=dtype, T=T, Hq=Hq, Hk=Hk, Hv=rng.choice([0, Hk]), D=D, rot=rng.choice([D, D, D // 2 // 16 * 16]), axes=rng.choice([1, 1, 3]),
+                    interleaved=rng.random() < 0.4, norm=rng.random() < 0.8)
+    D = rng.choice([32, 64, 64, 80, 96, 128, 128])
+    Hk = rng.choice([1, 2, 3, 4, 8])
+    Hq = Hk * rng.choice([1, 1, 2, 4, 7])
+    extra = dict(Hq=Hq, Hk=Hk, D=D, cap=rng.choice([0.0, 0.0, 30.0]), bias=rng.random() < 0.3, dtype=rng.choice(["f16", "bf16"]))
+    if op == "attend" and rng.random() < 0.4:   # few new tokens over a cache
+        Nq, Nk = rng.choice([1, 1, rng.randint(2, 40)]), _log(rng, 33, 16384)
+        Nk = max(Nk, Nq)
+        most = 16
+    else:
+        Nq = _log(rng, 1, 3500 if op == "attend" else 3000)
+        Nk = Nq + (rng.choice([0, 0, _log(rng, 1, 1000)]) if op == "attend" else 0)
+        most = max(1, min(64, (1 << 28) // (Nq * Nk * Hq)))
+    c = dict(op=op, B=_log(rng, 1, most), Nq=Nq, Nk=Nk, **mask, **extra)
+    return c if op == "attend" else dict(c, codes=rng.choice(["v", "v", "qkv", ""]))
+
+
+# ------------------------------------------------------------------------------------------------------- masks on the host
+def _lists(case):
+    """lengths, places of the first query, prefixes and documents of the sequences, as int32 arrays (None: not used)"""
+    B, Nq, Nk = case["B"], case["Nq"], case["Nk"]
+    r = random.Random("%d %d %d %d" % (B, Nq, Nk, case["docs"]))
+    length = np.array([r.randint(max(Nq, Nk // 2), Nk) if case["pad"] else Nk for _ in range(B)], np.int32)
+    start = (length - Nq).astype(np.int32) if Nq != Nk else np.zeros(B, np.int32)
+    prefix = np.array([r.randint(0, max(1, Nk // 8)) for _ in range(B)], np.int32) if case["prefix"] else None
+    doc = None
+    if case["docs"]:
+        cuts = np.zeros((B, Nk), np.int32)
+        for b in range(B):
+            for _ in range(case["docs"] - 1):
+                cuts[b, r.randrange(Nk)] += 1
+        doc = np.cumsum(cuts, axis=1, dtype=np.int32)
+    return length, start, prefix, doc
+
+
+def _intervals(case):
+    """lo, hi (B, Nq) in 64 bits on the host, from the definition: query i of sequence b has the place p = start + i and sees
+    the keys below the length; with a causal order those up to p, and those of the prefix; with a window w those nearer than w;
+    with documents those of its own. A query that is not in its sequence, or sees nothing, has 0, 0."""
+    length, start, prefix, doc = (None if a is None else a.astype(np.int64) for a in _lists(case))
+    B, Nq, Nk = case["B"], case["Nq"], case["Nk"]
+    p = start[:, None] + np.arange(Nq)[None, :]
+    n = length[:, None] + 0 * p
+    lo, hi = 0 * p, n.copy()
+    if case["causal"]:
+        hi = np.minimum(hi, np.maximum(p + 1, 0 if prefix is None else prefix[:, None]))
+    if case["window"]:
+        lo = np.maximum(lo, p - case["window"] + 1)
+        if not case["causal"]:
+            hi = np.minimum(hi, p + case["window"])
+    if doc is not None:
+        for b in range(B):
+            mine = doc[b, np.clip(p[b], 0, Nk - 1)]
+            lo[b] = np.maximum(lo[b], np.searchsorted(doc[b], mine, "left"))
+            hi[b] = np.minimum(hi[b], np.searchsorted(doc[b], mine, "right"))
+    none = (p < 0) | (p >= n) | (lo >= hi)
+    return np.where(none, 0, lo), np.where(none, 0, hi)
+
+
+# ---------------------------------------------------------------------------------------------------------------- inputs
+def _gpu(a):
+    return None if a is None else torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+
+
+def _normal(g, *shape):
+    return torch.randn(*shape, generator=g, device=DEV)
+
+
+def _codes(x, heads):
+    """codes (int8) of x (..., heads, D) with estimates that cut off the outermost values, and those estimates"""
+    rows = x.float().transpose(-2, -3).reshape(-1, heads, x.shape[-3], x.shape[-1]).transpose(0, 1).reshape(heads, -1)
+    mn, mx = 0.97 * rows.amin(1), 0.97 * rows.amax(1)
+    alpha, beta = (mx - mn).contiguous(), mn.contiguous()
+    q = (torch.round((x.float() - beta[:, None]) * (255.0 / alpha)[:, None]).clamp(0, 255) - 128).to(torch.int8)
+    return q, alpha, beta
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV).manual_seed(int(seed) * 7919 + 17)
+    s = dict(case=case)
+    if case["op"] == "bounds":
+        # the lists come from the case, shortened by the seed, so that other seeds are other inputs
+        length, start, prefix, doc = _lists(case)
+        s.update(length=_gpu(length), start=_gpu(start), prefix=_gpu(prefix), doc=_gpu(doc))
+        if case["pad"] or seed % 2:
+            s["length"] = torch.maximum(s["length"] - torch.randint(0, 3, (case["B"],), generator=g, device=DEV, dtype=torch.int32), s["length"] // 2)
+        s["lo"], s["hi"] = (torch.empty(case["B"], case["Nq"], dtype=torch.int32, device=DEV) for _ in range(2))
+        return s
+    dt = DTYPES[case["dtype"]]
+    D = case["D"]
+    if case["op"] in ("rope", "rope_bwd"):
+        T, Hq, Hk, Hv, rot = (case[k] for k in ("T", "Hq", "Hk", "Hv", "rot"))
+        H = Hq + Hk + Hv
+        x = _normal(g, T, H, D) * torch.exp(_normal(g, H, 1) * 0.5) + 0.2 * _normal(g, H, D)
+        x = torch.where(torch.rand(T, H, D, generator=g, device=DEV) < 0.001, 20 * x, x).to(dt)
+        s["x"] = x.reshape(T, H * D)
+        q, alpha, beta = _codes(x, H)
+        s["est"] = torch.stack([alpha, beta])
+        s["gamma"] = [(1 + 0.2 * _normal(g, D)).to(dt) for _ in range(2)] if case["norm"] else [None, None]
+        s["freq"] = torch.tensor([10000.0 ** (-2.0 * i / rot) for i in range(rot // 2)], dtype=torch.float32, device=DEV)
+        top = 1 << 17 if case["axes"] == 1 else 64
+        s["pos"] = torch.randint(0, top, (case["axes"], T), generator=g, device=DEV, dtype=torch.int32)
+        s["rstd"] = torch.empty(T, Hq + Hk, device=DEV)
+        s["q"] = torch.empty(T, H, D, dtype=torch.int8, device=DEV)
+        s["y"] = torch.empty(T, Hq + Hk, D, dtype=dt, device=DEV)
+        if case["op"] == "rope_bwd":
+            s["q"] = q
+            s["rstd"] = (x[:, :Hq + Hk].double().square().mean(-1) + EPS).rsqrt().float()
+            s["dy"] = _normal(g, T, Hq + Hk, D).to(dt)
+            s["dx"] = torch.empty(T, Hq + Hk, D, dtype=dt, device=DEV)
+            s["dgamma"] = [torch.empty(D, device=DEV) for _ in range(2)]
+        return s
+    B, Nq, Nk, Hq, Hk = (case[k] for k in ("B", "Nq", "Nk", "Hq", "Hk"))
+    lo, hi = _intervals(case)
+    s["lo"], s["hi"] = _gpu(lo.astype(np.int32)), _gpu(hi.astype(np.int32))
+    s["start"] = _gpu(_lists(case)[1])
+    s["slopes"] = torch.tensor([2.0 ** (-8.0 * (h + 1) / Hq) for h in range(Hq)], device=DEV) if case["bias"] else None
+    s["scale"] = D ** -0.5
+    # queries and keys as a norm for each head leaves them, with a spread of its own for each; values as a projection gives them
+    if Nq == Nk:   # packed: the heads of a token side by side
+        qk = (_normal(g, B, Nq, Hq + Hk, D) * torch.exp(0.3 * _normal(g, Hq + Hk, 1)))
+        qk = qk.to(dt)
+        q, k = qk[:, :, :Hq], qk[:, :, Hq:]
+    else:
+        q = (_normal(g, B, Nq, Hq, D) * torch.exp(0.3 * _normal(g, Hq, 1))).to(dt)
+        k = (_normal(g, B, Nk, Hk, D) * torch.exp(0.3 * _normal(g, Hk, 1))).to(dt)
+    v = (_normal(g, B, Nk, Hk, D) + 0.3 * _normal(g, Hk, D)).to(dt)
+    s.update(q=q, k=k, v=v)
+    s["o"] = torch.empty(B, Nq, Hq, D, dtype=dt, device=DEV)
+    s["lse"] = torch.empty(B, Hq, Nq, device=DEV)
+    if case["op"] == "attend_bwd":
+        o, lse = _attend(s)
+        s["o"], s["lse"] = o, lse
+        s["do"] = _normal(g, B, Nq, Hq, D).to(dt)
+        for name, heads in (("q", Hq), ("k", Hk), ("v", Hk)):
+            if name in case["codes"]:
+                s[name] = _codes(s[name], heads)
+                if case["codes"] == "qkv":   # head-wise, as (B, heads, tokens, D) lies in memory
+                    s[name] = (s[name][0].transpose(1, 2).contiguous().transpose(1, 2), *s[name][1:])
+        d = torch.empty(B, Nq, Hq + Hk, D, dtype=dt, device=DEV)
+        s["dq"], s["dk"], s["dv"] = d[:, :, :Hq], d[:, :, Hq:], torch.empty(B, Nk, Hk, D, dtype=dt, device=DEV)
+    return s
+
+
+# ------------------------------------------------------------------------------------------------------------ plain forms
+def _bounds(s):
+    c = s["case"]
+    length, start, prefix, doc = (None if t is None else t.long() for t in (s["length"], s["start"], s["prefix"], s["doc"]))
+    p = start[:, None] + torch.arange(c["Nq"], device=DEV)
+    n = length[:, None]
+    lo, hi = torch.zeros_like(p), n.expand_as(p)
+    if c["causal"]:
+        seen = p + 1 if prefix is None else torch.maximum(p + 1, prefix[:, None])
+        hi = torch.minimum(hi, seen)
+    if c["window"]:
+        lo = (p - c["window"] + 1).clamp_min(0)
+        if not c["causal"]:
+            hi = torch.minimum(hi, p + c["window"])
+    if doc is not None:
+        j = torch.arange(c["Nk"], device=DEV).expand_as(doc)
+        change = doc[:, 1:] != doc[:, :-1]
+        edge = torch.ones_like(doc[:, :1], dtype=torch.bool)
+        first = torch.where(torch.cat([edge, change], 1), j, 0).cummax(1).values
+        last = torch.where(torch.cat([change, edge], 1), j + 1, c["Nk"]).flip(1).cummin(1).values.flip(1)
+        at = p.clamp(0, c["Nk"] - 1)
+        lo, hi = torch.maximum(lo, first.gather(1, at)), torch.minimum(hi, last.gather(1, at))
+    none = (p < 0) | (p >= n) | (lo >= hi)
+    return {"lo": torch.where(none, 0, lo).int(), "hi": torch.where(none, 0, hi).int()}
+
+
+def _angles(s):
+    """cosine and sine (T, 1, rot/2) of position times frequency; the angles in 64 bits"""
+    c = s["case"]
+    half = c["rot"] // 2
+    part = -(-half // c["axes"])
+    axis = torch.arange(half, device=DEV) // part
+    a = s["pos"].double()[axis].t() * s["freq"].double()
+    return a.cos().float()[:, None], a.sin().float()[:, None]
+
+
+def _turn(z, cos, sin, interleaved):
+    rot = 2 * cos.shape[-1]
+    a, b = (z[..., 0:rot:2], z[..., 1:rot:2]) if interleaved else (z[..., :rot // 2], z[..., rot // 2:rot])
+    u, w = a * cos - b * sin, b * cos + a * sin
+    turned = torch.stack([u, w], -1).flatten(-2) if interleaved else torch.cat([u, w], -1)
+    return torch.cat([turned, z[..., rot:]], -1)
+
+
+def _gains(s):
+    c = s["case"]
+    return torch.cat([s["gamma"][0].float().expand(c["Hq"], -1), s["gamma"][1].float().expand(c["Hk"], -1)])
+
+
+def _rope(s):
+    c = s["case"]
+    T, Hq, Hk, Hv, D = (c[k] for k in ("T", "Hq", "Hk", "Hv", "D"))
+    x = s["x"].float().reshape(T, Hq + Hk + Hv, D)
+    alpha, beta = s["est"][0], s["est"][1]
+    codes = (torch.round((x - beta[:, None]) * (255.0 / alpha)[:, None]).clamp(0, 255) - 128).to(torch.int8)
+    mn, mx = x.amin((0, 2)), x.amax((0, 2))
+    keep, move = torch.tensor(LAM, device=DEV), 1 - torch.tensor(LAM, device=DEV)
+    out = {"q": codes, "alpha": keep * alpha + move * (mx - mn), "beta": keep * beta + move * mn}
+    z = x[:, :Hq + Hk]
+    if c["norm"]:
+        out["rstd"] = 1 / (z.square().mean(-1) + EPS).sqrt()
+        z = z * out["rstd"][..., None] * _gains(s)
+    out["y"] = _turn(z, *_angles(s), c["interleaved"]).to(s["x"].dtype)
+    return out
+
+
+def _hat(q, alpha, beta):
+    return (q.float() + 128) * (alpha / 255)[:, None] + beta[:, None]
+
+
+def _rope_bwd(s):
+    c = s["case"]
+    heads = c["Hq"] + c["Hk"]
+    cos, sin = _angles(s)
+    x = _hat(s["q"], s["est"][0], s["est"][1])[:, :heads]
+    g = _turn(s["dy"].float(), cos, -sin, c["interleaved"])
+    if not c["norm"]:
+        return {"y": _turn(x, cos, sin, c["interleaved"]).to(s["dy"].dtype), "dx": g.to(s["dy"].dtype)}
+    r = s["rstd"][..., None]
+    n, gain = x * r, _gains(s)
+    by_head = (g * n).double().sum(0)
+    h = g * gain
+    dx = r * (h - n * (h * n).mean(-1, keepdim=True))
+    return {"y": _turn(n * gain, cos, sin, c["interleaved"]).to(s["dy"].dtype), "dx": dx.to(s["dy"].dtype),
+            "dgamma_q": by_head[:c["Hq"]].sum(0).float(), "dgamma_k": by_head[c["Hq"]:].sum(0).float()}
+
+
+def _operand(x, dt):
+    """a tensor as it is, or codes with their estimates, de-quantized and rounded to the storage type; (B, heads, tokens, D) in 32 bits"""
+    x = x if torch.is_tensor(x) else _hat(*x).to(dt)
+    return x.float().transpose(1, 2)
+
+
+def _scores(s, q, k):
+    """the scores (B, Hq, Nq, Nk) of queries and keys in 32 bits, with the cap's slope where there is a cap, and what is seen"""
+    c = s["case"]
+    x = (q @ k.transpose(-1, -2)) * s["scale"]
+    slope = None
+    if c["cap"]:
+        t = torch.tanh(x / c["cap"])
+        x, slope = t * c["cap"], 1 - t * t
+    j = torch.arange(c["Nk"], device=DEV, dtype=torch.int32)
+    if s["slopes"] is not None:
+        p = s["start"][:, None] + torch.arange(c["Nq"], device=DEV)
+        far = (p[:, :, None] - j).abs()
+        x = x - s["slopes"][:, None, None] * far[:, None].float()
+    seen = (j >= s["lo"][..., None]) & (j < s["hi"][..., None])
+    return torch.where(seen[:, None], x, -math.inf), slope, seen[:, None]
+
+
+def _attend(s):
+    c = s["case"]
+    group = c["Hq"] // c["Hk"]
+    dt = DTYPES[c["dtype"]]
+    q, k, v = (_operand(s[n], dt) for n in ("q", "k", "v"))
+    x, _, _ = _scores(s, q, k.repeat_interleave(group, 1))
+    top = x.amax(-1, keepdim=True)
+    top = torch.where(top == -math.inf, 0.0, top)
+    e = torch.exp(x - top)
+    total = e.sum(-1, keepdim=True)
+    o = (e @ v.repeat_interleave(group, 1)) / torch.where(total == 0, 1.0, total)
+    return o.to(dt).transpose(1, 2).contiguous(), (top + torch.log(total))[..., 0]
+
+
+def _attend_bwd(s):
+    c = s["case"]
+    B, Nq, Nk, Hq, Hk, D = (c[k] for k in ("B", "Nq", "Nk", "Hq", "Hk", "D"))
+    group = Hq // Hk
+    dt = DTYPES[c["dtype"]]
+    q, k, v = (_operand(s[n], dt) for n in ("q", "k", "v"))
+    k, v = k.repeat_interleave(group, 1), v.repeat_interleave(group, 1)
+    o, do = s["o"].float().transpose(1, 2), s["do"].float().transpose(1, 2)
+    x, slope, seen = _scores(s, q, k)
+    p = torch.where(seen, torch.exp(x - s["lse"][..., None]), 0.0)
+    del x
+    ds = p * (do @ v.transpose(-1, -2) - (do * o).sum(-1, keepdim=True))
+    if slope is not None:
+        ds = ds * slope
+    dq = (ds @ k) * s["scale"]
+    dk = (ds.transpose(-1, -2) @ q) * s["scale"]
+    dv = p.transpose(-1, -2) @ do
+    dk, dv = (t.reshape(B, Hk, group, Nk, D).sum(2) for t in (dk, dv))
+    return {n: t.to(dt).transpose(1, 2) for n, t in (("dq", dq), ("dk", dk), ("dv", dv))}
+
+
+# ------------------------------------------------------------------------------------------------------- the library's calls
+def _own(s):
+    import paper_2111_11124_amd as m
+
+    c = s["case"]
+    op = c["op"]
+    if op == "bounds":
+        m.mesa_attention_bounds(s["lo"], s["hi"], c["Nk"], c["causal"], c["window"], kv_len=s["length"], q_start=s["start"], prefix=s["prefix"], doc=s["doc"])
+        return {"lo": s["lo"], "hi": s["hi"]}
+    dt = {"f16": m.F16, "bf16": m.BF16, "f32": m.F32}[c["dtype"]]
+    if op in ("rope", "rope_bwd"):
+        if "geom" not in s:   # once per layer: the heads' description and a workspace
+            half = c["rot"] // 2
+            part = -(-half // c["axes"])
+            sections = [max(0, min(part, half - a * part)) for a in range(c["axes"])]
+            s["geom"] = m.QkvHeads(c["T"], c["Hq"], c["Hk"], c["Hv"], c["D"], c["rot"], c["interleaved"], sections, EPS)
+            size = (m.qkv_norm_rope_fwd_q_workspace_bytes if op == "rope" else m.qkv_norm_rope_bwd_q_workspace_bytes)(s["geom"], dt)
+            s["ws"] = torch.empty(max(16, size), dtype=torch.uint8, device=DEV)
+        gq, gk = s["gamma"]
+        if op == "rope":
+            est = s["est"].clone()
+            m.mesa_qkv_norm_rope_fwd_q(s["x"], s["geom"], gq, gk, s["freq"], s["pos"], est[0], est[1], LAM, s["y"], s["rstd"] if c["norm"] else None, s["q"], s["ws"],
+                                       m.ROUND_NEAREST_EVEN)
+            out = {"q": s["q"], "alpha": est[0], "beta": est[1], "y": s["y"]}
+            return dict(out, rstd=s["rstd"]) if c["norm"] else out
+        rstd = s["rstd"] if c["norm"] else None
+        dgq, dgk = s["dgamma"] if c["norm"] else (None, None)
+        m.mesa_qkv_norm_rope_recompute_q(s["q"], s["geom"], gq, gk, s["freq"], s["pos"], s["est"][0], s["est"][1], rstd, s["y"])
+        m.mesa_qkv_norm_rope_bwd_q(s["q"], s["geom"], gq, gk, s["freq"], s["pos"], s["est"][0], s["est"][1], rstd, s["dy"], s["dx"], dgq, dgk, s["ws"])
+        out = {"y": s["y"], "dx": s["dx"]}
+        return dict(out, dgamma_q=dgq, dgamma_k=dgk) if c["norm"] else out
+    if "plan" not in s:       # once per layer: the shape and a workspace
+        s["plan"] = m.Attention(c["B"], c["Nq"], c["Nk"], c["Hq"], c["Hk"], c["D"], s["scale"], c["cap"])
+        coded = c.get("codes", "")
+        size = m.attention_fwd_workspace_bytes(s["plan"], dt) if op == "attend" else m.attention_bwd_q_workspace_bytes(s["plan"], "q" in coded, "k" in coded, "v" in coded, dt)
+        s["ws"] = torch.empty(max(16, size), dtype=torch.uint8, device=DEV)
+    if op == "attend":
+        m.mesa_attention_fwd(s["plan"], s["q"], s["k"], s["v"], s["o"], s["lse"], s["ws"], lo=s["lo"], hi=s["hi"], slopes=s["slopes"], q_start=s["start"])
+        return {"o": s["o"], "lse": s["lse"]}
+    m.mesa_attention_bwd_q(s["plan"], s["q"], s["k"], s["v"], s["o"], s["lse"], s["do"], s["dq"], s["dk"], s["dv"], s["ws"], lo=s["lo"], hi=s["hi"], slopes=s["slopes"],
+                           q_start=s["start"])
+    return {"dq": s["dq"], "dk": s["dk"], "dv": s["dv"]}
+
+
+def run(state):
+    if own:
+        return _own(state)
+    op = state["case"]["op"]
+    if op == "attend":
+        o, lse = _attend(state)
+        return {"o": o, "lse": lse}
+    return {"bounds": _bounds, "rope": _rope, "rope_bwd": _rope_bwd, "attend_bwd": _attend_bwd}[op](state)
+
+
+# ------------------------------------------------------------------------------------------------------------------- work
+def work(case):
+    if case["op"] == "bounds":
+        lists = 2 + bool(case["prefix"]) + (case["Nk"] if case["docs"] else 0)
+        return {"bytes": 4 * case["B"] * (2 * case["Nq"] + lists), "flops": 0}
+    size = 4 if case["dtype"] == "f32" else 2
+    if case["op"] in ("rope", "rope_bwd"):
+        T, D, turned = case["T"], case["D"], case["Hq"] + case["Hk"]
+        every = turned + case["Hv"]
+        rest = 4 * T * case["axes"] + 2 * case["rot"] + (4 * T * turned if case["norm"] else 0)
+        if case["op"] == "rope":   # the projection in; queries, keys and codes out
+            return {"bytes": T * D * (every * (size + 1) + turned * size) + rest, "flops": 12 * T * turned * D}
+        return {"bytes": T * D * turned * (1 + 3 * size) + rest, "flops": 24 * T * turned * D}   # codes and dy in; queries and keys, dx out
+    lo, hi = _intervals(case)
+    pairs = int((hi - lo).sum()) * case["Hq"]
+    B, Nq, Nk, Hq, Hk, D = (case[k] for k in ("B", "Nq", "Nk", "Hq", "Hk", "D"))
+    seen = min(B * Nk, int(hi.max(axis=1).sum()))   # rows of keys that some query sees
+    rows, keys = B * Nq * Hq * D, seen * Hk * D
+    if case["op"] == "attend":
+        return {"bytes": 2 * (2 * rows + 2 * keys) + 4 * B * Hq * Nq + 8 * B * Nq, "flops": 4 * D * pairs}
+    wide = [1 if n in case["codes"] else 2 for n in "qkv"]
+    return {"bytes": rows * (wide[0] + 6) + keys * (wide[1] + wide[2] + 4) + 4 * B * Hq * Nq + 8 * B * Nq, "flops": 10 * D * pairs}
+
+
+# ------------------------------------------------------------------------------------------------------------------ 64 bits
+def exact(case, seed):
+    s = prepare(case, seed)
+    op = case["op"]
+    if op == "bounds":
+        return None       # whole numbers
+    f8 = torch.float64
+    if op in ("rope", "rope_bwd"):
+        T, Hq, Hk, Hv, D, rot = (case[k] for k in ("T", "Hq", "Hk", "Hv", "D", "rot"))
+        n, H, half = Hq + Hk, Hq + Hk + Hv, rot // 2
+        part = -(-half // case["axes"])
+        angle = torch.empty(T, half, dtype=f8, device=DEV)
+        for i in range(half):
+            angle[:, i] = s["pos"][i // part].to(f8) * s["freq"][i].to(f8)
+        e = torch.complex(angle.cos(), angle.sin())[:, None]
+
+        def spin(z, by):      # the rotation as a product of complex numbers
+            z = z.clone()
+            first, second = (slice(0, rot, 2), slice(1, rot, 2)) if case["interleaved"] else (slice(0, half), slice(half, rot))
+            w = torch.complex(z[..., first], z[..., second]) * by
+            z[..., first], z[..., second] = w.real, w.imag
+            return z
+
+        gain = torch.ones(n, D, dtype=f8, device=DEV)
+        if case["norm"]:
+            gain[:Hq], gain[Hq:] = s["gamma"][0].to(f8), s["gamma"][1].to(f8)
+        alpha, beta = s["est"].to(f8)
+        if op == "rope":
+            x = s["x"].to(f8).reshape(T, H, D)
+            one = lambda t: t.float().to(f8)  # noqa: E731  codes are defined by binary32 operations, each rounded by itself
+            codes = torch.round(one(one(x - beta[:, None]) * one(255 / alpha)[:, None])).clamp(0, 255) - 128
+            lam = float(np.float32(LAM))
+            mn, mx = x.amin((0, 2)), x.amax((0, 2))
+            out = {"q": codes.to(torch.int8), "alpha": lam * alpha + (1 - lam) * (mx - mn), "beta": lam * beta + (1 - lam) * mn}
+            z = x[:, :n]
+            if case["norm"]:
+                out["rstd"] = ((z * z).sum(-1) / D + EPS) ** -0.5
+                z = z * out["rstd"][..., None] * gain
+            return dict(out, y=spin(z, e))
+        x = (s["q"][:, :n].to(f8) + 128) * (alpha[:n] / 255)[:, None] + beta[:n, None]
+        back = spin(s["dy"].to(f8), e.conj())
+        if not case["norm"]:
+            return {"y": spin(x, e), "dx": back}
+        r = s["rstd"].to(f8)[..., None]
+        unit = x * r
+        dgain = (back * unit).sum(0)
+        h = back * gain
+        dx = (h - unit * ((h * unit).sum(-1, keepdim=True) / D)) * r
+        return {"y": spin(unit * gain, e), "dx": dx, "dgamma_q": dgain[:Hq].sum(0), "dgamma_k": dgain[Hq:].sum(0)}
+    B, Nq, Nk, Hq, Hk, D = (case[k] for k in ("B", "Nq", "Nk", "Hq", "Hk", "D"))
+    dt = DTYPES[case["dtype"]]
+    lo, hi = (torch.from_numpy(a).to(DEV) for a in _intervals(case))
+
+    def load(x):              # the operand in the storage type, then in 64 bits
+        if not torch.is_tensor(x):
+            codes, alpha, beta = x
+            x = ((codes.float() + 128) * (alpha / 255)[:, None] + beta[:, None]).to(dt)
+        return x
+
+    q, k, v = load(s["q"]), load(s["k"]), load(s["v"])
+    names = ("o", "lse") if op == "attend" else ("dq", "dk", "dv")
+    shapes = ((B, Nq, Hq, D), (B, Hq, Nq)) if op == "attend" else ((B, Nq, Hq, D), (B, Nk, Hk, D), (B, Nk, Hk, D))
+    out = {n: torch.zeros(sh, dtype=f8, device=DEV) for n, sh in zip(names, shapes)}
+    j = torch.arange(Nk, device=DEV)
+    for b in range(B):
+        hidden = ~((j[None] >= lo[b][:, None]) & (j[None] < hi[b][:, None]))
+        far = (int(s["start"][b]) + torch.arange(Nq, device=DEV)[:, None] - j[None]).abs().to(f8)
+        for h in range(Hq):
+            kv = h // (Hq // Hk)
+            Q, K, V = q[b, :, h].to(f8), k[b, :, kv].to(f8), v[b, :, kv].to(f8)
+            x = torch.mm(Q, K.t().contiguous()) * s["scale"]
+            if case["cap"]:
+                t = torch.tanh(x / case["cap"])
+                x = case["cap"] * t
+            if case["bias"]:
+                x = x - float(s["slopes"][h]) * far
+            x = x.masked_fill(hidden, -math.inf)
+            if op == "attend":
+                lse = torch.logsumexp(x, -1)
+                out["lse"][b, h] = lse
+                p = torch.exp(x - lse.masked_fill(lse == -math.inf, 0)[:, None])
+                out["o"][b, :, h] = p @ V
+                continue
+            dO = s["do"][b, :, h].to(f8)
+            p = torch.exp(x - s["lse"][b, h].to(f8)[:, None]).masked_fill(hidden, 0)
+            ds = p * (torch.mm(dO, V.t().contiguous()) - (dO * s["o"][b, :, h].to(f8)).sum(-1)[:, None])
+            if case["cap"]:
+                ds = ds * (1 - t * t)
+            out["dv"][b, :, kv] += torch.mm(p.t().contiguous(), dO)
+            out["dk"][b, :, kv] += torch.mm(ds.t().contiguous(), Q) * s["scale"]
+            out["dq"][b, :, h] = torch.mm(ds, K) * s["scale"]
+    return out
