@@ -154,12 +154,18 @@ def _normal(g, *shape):
     return torch.randn(*shape, generator=g, device=DEV)
 
 
+def _over(a, b):
+    """a / b element by element, rounded once; a division by or of a plain number would go by way of a rounded reciprocal"""
+    a, b = (t if torch.is_tensor(t) else torch.full_like(o, t) for t, o in ((a, b), (b, a)))
+    return a / b
+
+
 def _codes(x, heads):
     """codes (int8) of x (..., heads, D) with estimates that cut off the outermost values, and those estimates"""
     rows = x.float().transpose(-2, -3).reshape(-1, heads, x.shape[-3], x.shape[-1]).transpose(0, 1).reshape(heads, -1)
     mn, mx = 0.97 * rows.amin(1), 0.97 * rows.amax(1)
     alpha, beta = (mx - mn).contiguous(), mn.contiguous()
-    q = (torch.round((x.float() - beta[:, None]) * (255.0 / alpha)[:, None]).clamp(0, 255) - 128).to(torch.int8)
+    q = (torch.round((x.float() - beta[:, None]) * _over(255.0, alpha)[:, None]).clamp(0, 255) - 128).to(torch.int8)
     return q, alpha, beta
 
 
@@ -284,7 +290,7 @@ def _rope(s):
     T, Hq, Hk, Hv, D = (c[k] for k in ("T", "Hq", "Hk", "Hv", "D"))
     x = s["x"].float().reshape(T, Hq + Hk + Hv, D)
     alpha, beta = s["est"][0], s["est"][1]
-    codes = (torch.round((x - beta[:, None]) * (255.0 / alpha)[:, None]).clamp(0, 255) - 128).to(torch.int8)
+    codes = (torch.round((x - beta[:, None]) * _over(255.0, alpha)[:, None]).clamp(0, 255) - 128).to(torch.int8)
     mn, mx = x.amin((0, 2)), x.amax((0, 2))
     keep, move = torch.tensor(LAM, device=DEV), 1 - torch.tensor(LAM, device=DEV)
     out = {"q": codes, "alpha": keep * alpha + move * (mx - mn), "beta": keep * beta + move * mn}
@@ -297,7 +303,7 @@ def _rope(s):
 
 
 def _hat(q, alpha, beta):
-    return (q.float() + 128) * (alpha / 255)[:, None] + beta[:, None]
+    return (q.float() + 128) * _over(alpha, 255.0)[:, None] + beta[:, None]
 
 
 def _rope_bwd(s):
@@ -483,7 +489,7 @@ def exact(case, seed):
         if op == "rope":
             x = s["x"].to(f8).reshape(T, H, D)
             one = lambda t: t.float().to(f8)  # noqa: E731  codes are defined by binary32 operations, each rounded by itself
-            codes = torch.round(one(one(x - beta[:, None]) * one(255 / alpha)[:, None])).clamp(0, 255) - 128
+            codes = torch.round(one(one(x - beta[:, None]) * one(_over(255.0, alpha))[:, None])).clamp(0, 255) - 128
             lam = float(np.float32(LAM))
             mn, mx = x.amin((0, 2)), x.amax((0, 2))
             out = {"q": codes.to(torch.int8), "alpha": lam * alpha + (1 - lam) * (mx - mn), "beta": lam * beta + (1 - lam) * mn}
@@ -509,7 +515,7 @@ def exact(case, seed):
     def load(x):              # the operand in the storage type, then in 64 bits
         if not torch.is_tensor(x):
             codes, alpha, beta = x
-            x = ((codes.float() + 128) * (alpha / 255)[:, None] + beta[:, None]).to(dt)
+            x = ((codes.float() + 128) * _over(alpha, 255.0)[:, None] + beta[:, None]).to(dt)
         return x
 
     q, k, v = load(s["q"]), load(s["k"]), load(s["v"])
