@@ -382,6 +382,132 @@ mesa_status mesa_attn_qk_bwd_q(const int8_t *qq, const int8_t *kq, int64_t B, in
                                const float *alpha_q, const float *beta_q, const float *alpha_k, const float *beta_k,
                                const void *dS, float scale, void *dQ, void *dK, mesa_dtype dt, void *stream);
 
+/*
+ * The attention block of a language model.  A token's queries, keys and values come out of one projection, heads side by
+ * side; queries and keys get a norm for each head and a rotation by position; query heads share key heads; and the mask is
+ * an interval of keys per query (causal order, windows, prefixes, packed documents, padded batches).  The layer saves the
+ * projection as codes, one (alpha, beta) pair per head, and nothing else but rstd and the attention's log-sum-exp: its
+ * backward makes queries and keys again from the codes.
+ *
+ *   forward    mesa_qkv_norm_rope_fwd_q -> mesa_attention_fwd
+ *   backward   mesa_qkv_norm_rope_recompute_q -> mesa_attention_bwd_q (values straight from the codes) -> mesa_qkv_norm_rope_bwd_q
+ */
+
+/*
+ * The heads of such a projection.  x has T rows (tokens) of Hq query, Hk key and Hv value heads of D elements each; Hq + Hk
+ * heads are normed and rotated, the value heads are only saved.
+ *   norm      r = 1 / sqrt(sum_d x_d^2 / D + eps),  z_d = gamma_d * x_d * r    (gamma_q for query heads, gamma_k for key heads;
+ *             both NULL: no norm, z = x)
+ *   rotation  of the first `rot` elements of a head: pair i (i < rot/2) is turned by the angle pos[axis(i)][t] * freq[i],
+ *               y_a = z_a cos - z_b sin,  y_b = z_b cos + z_a sin      with (a, b) = (i, i + rot/2), or (2i, 2i + 1) if interleaved
+ *             axis(i): section[0] pairs belong to the first row of pos, the next section[1] to the second, and so on.  The angle
+ *             is formed and reduced in binary64.
+ * T >= 0; Hq + Hk >= 1; Hq + Hk + Hv <= 512; D a multiple of 8, 8 <= D <= 256; rot even, 0 <= rot <= D (rot = 0: no rotation;
+ * not interleaved: rot a multiple of 16); 1 <= axes <= 4, sections >= 0 with sum rot/2; eps >= 0.  Outside these ranges:
+ * MESA_ERR_INVALID_ARG for what contradicts itself, MESA_ERR_UNSUPPORTED for a D, rot or head count that the kernels do not take.
+ */
+typedef struct mesa_qkv_heads {
+    int64_t T, Hq, Hk, Hv, D, rot;
+    int32_t interleaved, axes;
+    int64_t section[4];
+    float eps;
+} mesa_qkv_heads;
+
+/*
+ * Forward, one pass over x:  y (T, Hq+Hk, D) contiguous, of dt;  rstd (T, Hq+Hk) binary32 (what the backward takes; NULL
+ * without a norm);  q (T, Hq+Hk+Hv, D) int8, codes of every head of x with alpha, beta as they are on entry, Eq. (3)-(4);
+ * alpha, beta [Hq+Hk+Hv] then moved by this batch's extrema, Eq. (6)-(7) -- bit for bit mesa_quantize_update_fused on x with the
+ * layout {T, Hq+Hk+Hv, D}.  Row t of x is at x + t*x_row elements (x_row a multiple of 8, >= (Hq+Hk+Hv)*D).
+ * gamma_q, gamma_k: [D] of dt.  freq: [rot/2] binary32.  pos: [axes][T] int32, any value.  x, y, q, gamma_* 16-byte aligned.
+ * ws: mesa_qkv_norm_rope_fwd_q_workspace_bytes(h, dt) bytes.
+ */
+size_t mesa_qkv_norm_rope_fwd_q_workspace_bytes(mesa_qkv_heads h, mesa_dtype dt);
+mesa_status mesa_qkv_norm_rope_fwd_q(const void *x, int64_t x_row, mesa_qkv_heads h, const void *gamma_q, const void *gamma_k,
+                                     const float *freq, const int32_t *pos, float *alpha, float *beta, float lambda,
+                                     void *y, float *rstd, int8_t *q, mesa_round mode, uint64_t seed, uint64_t offset,
+                                     void *ws, size_t ws_bytes, mesa_dtype dt, void *stream);
+/* y again, from the codes and the forward's rstd:  the forward's formulas at x_hat (Eq. (5), not rounded to dt). */
+mesa_status mesa_qkv_norm_rope_recompute_q(const int8_t *q, mesa_qkv_heads h, const void *gamma_q, const void *gamma_k,
+                                           const float *freq, const int32_t *pos, const float *alpha, const float *beta,
+                                           const float *rstd, void *y, mesa_dtype dt, void *stream);
+/*
+ * Backward at x_hat with the forward's rstd.  g = dy turned back; per head, n = x_hat * rstd, u = gamma * g:
+ *   dx = rstd * (u - n * mean_d(u*n)),   dgamma_q[d] = sum over tokens and query heads of g*n, dgamma_k likewise
+ * (without a norm dx = g; q, alpha, beta, rstd, dgamma_* are not used and may be NULL).
+ * dy (T, Hq+Hk, D) contiguous of dt.  Row t of dx is at dx + t*dx_row elements, Hq+Hk heads (dx_row a multiple of 8,
+ * >= (Hq+Hk)*D): rows of the projection's gradient, whose value heads stay as they are.  dx may alias dy where its rows are
+ * dy's.  dgamma_*: [D] binary32, overwritten, fixed summation order.  ws: mesa_qkv_norm_rope_bwd_q_workspace_bytes(h, dt) bytes.
+ */
+size_t mesa_qkv_norm_rope_bwd_q_workspace_bytes(mesa_qkv_heads h, mesa_dtype dt);
+mesa_status mesa_qkv_norm_rope_bwd_q(const int8_t *q, mesa_qkv_heads h, const void *gamma_q, const void *gamma_k,
+                                     const float *freq, const int32_t *pos, const float *alpha, const float *beta,
+                                     const float *rstd, const void *dy, void *dx, int64_t dx_row, float *dgamma_q, float *dgamma_k,
+                                     void *ws, size_t ws_bytes, mesa_dtype dt, void *stream);
+
+/*
+ * The interval of keys [lo, hi) that each query sees, for all layers and heads of a step.  Query i of sequence b has the place
+ * p = q_start[b] + i (q_start NULL: Nk - Nq + i) among that sequence's kv_len[b] keys (NULL: Nk; taken as at most Nk):
+ *   hi = kv_len;  causal: hi = min(kv_len, max(p + 1, prefix[b]))         (prefix NULL: none)
+ *   window > 0:   lo = p - window + 1;  not causal: hi = min(hi, p + window) too
+ *   doc (B, Nk):  lo, hi within the run of keys with doc[b][p]'s number; numbers do not decrease along a row
+ * lo = hi = 0 for a query without a place (p < 0 or p >= kv_len) or one that sees nothing.  Every result has 0 <= lo <= hi <= Nk,
+ * whatever the lists hold.
+ * lo, hi: (B, Nq) int32 (out).  kv_len, q_start, prefix: [B] int32.  0 <= Nq, Nk < 2^30; B*Nq < 2^40; window >= 0.
+ */
+mesa_status mesa_attention_bounds(int32_t *lo, int32_t *hi, int64_t B, int64_t Nq, int64_t Nk, int causal, int64_t window,
+                                  const int32_t *kv_len, const int32_t *q_start, const int32_t *prefix, const int32_t *doc,
+                                  void *stream);
+
+/*
+ * Attention without a map in memory.  Query head h reads key and value head h / (Hq/Hk):
+ *   s_ij = scale * q_i.k_j;   cap > 0: s = cap * tanh(s / cap);   slopes: s -= slopes[h] * |p_i - j|  (p_i as above)
+ *   over the keys lo[b][i] <= j < hi[b][i] (cut to [0, Nk); lo and hi NULL: all):  p = softmax(s),  o_i = sum_j p_ij v_j
+ *   lse_i = log sum_j exp(s_ij)   (binary32, (B, Hq, Nq))
+ * A query that sees nothing gets o = 0, lse = -infinity and no gradients.  What rows of k and v hold that no query of their
+ * sequence sees, and rows of q, o and do whose query sees nothing, does not matter (infinities and NaN neither).
+ * Storage is binary16 or bfloat16; scores, softmax and sums are binary32, the probabilities that enter a product are rounded to dt.
+ * 1 <= Hk, Hq a multiple of Hk; D a multiple of 8, 8 <= D <= 128, else MESA_ERR_UNSUPPORTED (MESA_F32 too).
+ * Nq, Nk < 2^30, Nq * (Hq/Hk) < 2^31; scale > 0 and cap >= 0, finite.  Nk = 0: o = 0, lse = -infinity.
+ */
+typedef struct mesa_attention {
+    int64_t B, Nq, Nk, Hq, Hk, D;
+    float scale, cap;
+} mesa_attention;
+typedef struct mesa_attention_mask {
+    const int32_t *lo, *hi;      /* (B, Nq), both or neither */
+    const float *slopes;         /* [Hq] or NULL */
+    const int32_t *q_start;      /* [B] or NULL: Nk - Nq */
+} mesa_attention_mask;
+/* (B, tokens, heads, D) in memory: element (b, t, h, d) at b*batch + t*token + h*head + d.  Strides are multiples of 8, data is
+ * 16-byte aligned, and the heads of a group and 256 tokens span less than 2^30 elements.  alpha NULL: elements of dt.  Else
+ * codes, de-quantized to dt as mesa_dequantize does, with [heads] binary32 alpha and beta (data 8-byte aligned then). */
+typedef struct mesa_attention_in {
+    const void *data;
+    int64_t batch, token, head;
+    const float *alpha, *beta;
+} mesa_attention_in;
+typedef struct mesa_attention_out {
+    void *data;
+    int64_t batch, token, head;
+} mesa_attention_out;
+/* Forward.  q, k, v are of dt (codes: MESA_ERR_INVALID_ARG).  ws: mesa_attention_fwd_workspace_bytes(a, dt) bytes, 0 where it needs none. */
+size_t mesa_attention_fwd_workspace_bytes(mesa_attention a, mesa_dtype dt);
+mesa_status mesa_attention_fwd(mesa_attention a, mesa_attention_in q, mesa_attention_in k, mesa_attention_in v,
+                               mesa_attention_out o, float *lse, mesa_attention_mask m, void *ws, size_t ws_bytes,
+                               mesa_dtype dt, void *stream);
+/*
+ * Backward, Eq. (2): the gradient function at the saved operands, each codes or (made again from codes) of dt, with the exact
+ * forward's output o and lse:   p = exp(s - lse),  delta_i = do_i.o_i,  ds = p * (do.v - delta) (times the cap's derivative),
+ *   dv_j = sum_i p_ij do_i,   dq_i = scale * sum_j ds_ij k_j,   dk_j = scale * sum_i ds_ij q_i   (over a group's heads too).
+ * dq, dk, dv are overwritten; keys that no query sees get 0.  Fixed summation order.  o, do: of dt (codes:
+ * MESA_ERR_INVALID_ARG).  ws: mesa_attention_bwd_q_workspace_bytes(a, q, k, v are codes, dt) bytes.
+ */
+size_t mesa_attention_bwd_q_workspace_bytes(mesa_attention a, int q_codes, int k_codes, int v_codes, mesa_dtype dt);
+mesa_status mesa_attention_bwd_q(mesa_attention a, mesa_attention_in q, mesa_attention_in k, mesa_attention_in v,
+                                 mesa_attention_in o, const float *lse, mesa_attention_in dO, mesa_attention_out dq,
+                                 mesa_attention_out dk, mesa_attention_out dv, mesa_attention_mask m, void *ws, size_t ws_bytes,
+                                 mesa_dtype dt, void *stream);
+
 /* Scratch size in bytes for `op` at the given extents (see mesa_op); 0 for unknown ops. */
 size_t mesa_workspace_bytes(mesa_op op, int64_t d0, int64_t d1, int64_t d2, mesa_dtype dt);
 

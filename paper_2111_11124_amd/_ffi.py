@@ -27,6 +27,9 @@ OP_UPDATE_RUNNING_PARAMS, OP_LAYERNORM_BWD_Q, OP_LINEAR_DW_Q, OP_SOFTMAX_FWD_Q, 
 EXPORTS = [
     "mesa_update_running_params", "mesa_update_running_params_sym", "mesa_update_running_params_fixed_beta", "mesa_update_running_scale_sym", "mesa_quantize_sym", "mesa_dequantize_sym", "mesa_update_running_params_static", "mesa_static_scratch_bytes", "mesa_quantize_headwise", "mesa_quantize_update_fused", "mesa_gelu_fwd_q", "mesa_softmax_fwd_q", "mesa_layernorm_fwd_q", "mesa_dequantize", "mesa_quantize_headwise_b4", "mesa_dequantize_b4", "mesa_gelu_bwd_q_b4", "mesa_softmax_bwd_q",
     "mesa_gelu_bwd_q", "mesa_relu_bwd_q", "mesa_layernorm_bwd_q", "mesa_linear_dw_q", "mesa_conv2d_dw_q", "mesa_conv2d_dw_q_workspace_bytes", "mesa_attn_av_bwd_q", "mesa_attn_qk_bwd_q",
+    "mesa_qkv_norm_rope_fwd_q", "mesa_qkv_norm_rope_fwd_q_workspace_bytes", "mesa_qkv_norm_rope_recompute_q", "mesa_qkv_norm_rope_bwd_q",
+    "mesa_qkv_norm_rope_bwd_q_workspace_bytes", "mesa_attention_bounds", "mesa_attention_fwd", "mesa_attention_fwd_workspace_bytes", "mesa_attention_bwd_q",
+    "mesa_attention_bwd_q_workspace_bytes",
     "mesa_workspace_bytes",
     "mesa_status_string", "mesa_version", "mesa_stream_copy", "mesa_stream_read", "mesa_stream_fill", "mesa_mfma_probe", "mesa_event_create", "mesa_event_record",
     "mesa_event_elapsed_ms", "mesa_event_destroy",
@@ -51,6 +54,39 @@ class Conv2d(C.Structure):
     def out_hw(self):
         return ((self.H + 2 * self.pad_h - self.dil_h * (self.KH - 1) - 1) // self.stride_h + 1,
                 (self.W + 2 * self.pad_w - self.dil_w * (self.KW - 1) - 1) // self.stride_w + 1)
+
+
+class QkvHeads(C.Structure):
+    """mesa_qkv_heads: the heads of a packed query/key/value projection; sections: pairs of elements turned by each row of positions"""
+    _fields_ = [("T", C.c_int64), ("Hq", C.c_int64), ("Hk", C.c_int64), ("Hv", C.c_int64), ("D", C.c_int64), ("rot", C.c_int64), ("interleaved", C.c_int32),
+                ("axes", C.c_int32), ("section", C.c_int64 * 4), ("eps", C.c_float)]
+
+    def __init__(self, T, Hq, Hk, Hv, D, rot=None, interleaved=False, sections=None, eps=1e-6):
+        rot = D if rot is None else rot
+        sections = [rot // 2] if sections is None else list(sections)
+        if not 1 <= len(sections) <= 4:
+            raise ValueError("one to four sections")
+        super().__init__(T, Hq, Hk, Hv, D, rot, int(bool(interleaved)), len(sections), (C.c_int64 * 4)(*sections), eps)
+
+
+class Attention(C.Structure):
+    """mesa_attention: the sizes of an attention, its scale and its cap (0: none)"""
+    _fields_ = [("B", C.c_int64), ("Nq", C.c_int64), ("Nk", C.c_int64), ("Hq", C.c_int64), ("Hk", C.c_int64), ("D", C.c_int64), ("scale", C.c_float), ("cap", C.c_float)]
+
+    def __init__(self, B, Nq, Nk, Hq, Hk, D, scale, cap=0.0):
+        super().__init__(B, Nq, Nk, Hq, Hk, D, scale, cap)
+
+
+class AttentionMask(C.Structure):
+    _fields_ = [("lo", C.c_void_p), ("hi", C.c_void_p), ("slopes", C.c_void_p), ("q_start", C.c_void_p)]
+
+
+class AttentionIn(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64), ("alpha", C.c_void_p), ("beta", C.c_void_p)]
+
+
+class AttentionOut(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
 
 
 _lib = None
@@ -129,9 +165,20 @@ def lib() -> C.CDLL:
         L.mesa_conv2d_dw_q.argtypes = [_vp, Conv2d, _i64, _vp, _vp, _vp, _int, _vp, _vp, _vp, _sz, _vp]
         L.mesa_conv2d_dw_q_workspace_bytes.argtypes = [Conv2d, _int]
         L.mesa_conv2d_dw_q_workspace_bytes.restype = _sz
+        L.mesa_qkv_norm_rope_fwd_q.argtypes = [_vp, _i64, QkvHeads, _vp, _vp, _vp, _vp, _vp, _vp, _f32, _vp, _vp, _vp, _int, _u64, _u64, _vp, _sz, _int, _vp]
+        L.mesa_qkv_norm_rope_recompute_q.argtypes = [_vp, QkvHeads, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _int, _vp]
+        L.mesa_qkv_norm_rope_bwd_q.argtypes = [_vp, QkvHeads, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _sz, _int, _vp]
+        L.mesa_attention_bounds.argtypes = [_vp, _vp, _i64, _i64, _i64, _int, _i64, _vp, _vp, _vp, _vp, _vp]
+        L.mesa_attention_fwd.argtypes = [Attention, AttentionIn, AttentionIn, AttentionIn, AttentionOut, _vp, AttentionMask, _vp, _sz, _int, _vp]
+        L.mesa_attention_bwd_q.argtypes = [Attention, AttentionIn, AttentionIn, AttentionIn, AttentionIn, _vp, AttentionIn, AttentionOut, AttentionOut, AttentionOut,
+                                           AttentionMask, _vp, _sz, _int, _vp]
+        for name, args in (("mesa_qkv_norm_rope_fwd_q_workspace_bytes", [QkvHeads, _int]), ("mesa_qkv_norm_rope_bwd_q_workspace_bytes", [QkvHeads, _int]),
+                           ("mesa_attention_fwd_workspace_bytes", [Attention, _int]), ("mesa_attention_bwd_q_workspace_bytes", [Attention, _int, _int, _int, _int])):
+            getattr(L, name).argtypes = args
+            getattr(L, name).restype = _sz
         for name in EXPORTS:
             fn = getattr(L, name)
-            if name not in ("mesa_workspace_bytes", "mesa_status_string", "mesa_version", "mesa_static_scratch_bytes",
+            if not name.endswith("_workspace_bytes") and name not in ("mesa_workspace_bytes", "mesa_status_string", "mesa_version", "mesa_static_scratch_bytes",
                             "mesa_conv2d_dw_q_workspace_bytes"):
                 fn.restype = _int
         if _fast is None:
@@ -430,6 +477,143 @@ def mesa_conv2d_dw_q(xq, cv: Conv2d, G, alpha, beta, dy, dW, db, ws):
                "mesa_conv2d_dw_q")
     elif st:
         _check(st, "mesa_conv2d_dw_q")
+
+
+# ---- a language model's attention block ----
+def qkv_norm_rope_fwd_q_workspace_bytes(heads: QkvHeads, dtype: int = F16) -> int:
+    return int(lib().mesa_qkv_norm_rope_fwd_q_workspace_bytes(heads, int(dtype)))
+
+
+def qkv_norm_rope_bwd_q_workspace_bytes(heads: QkvHeads, dtype: int = F16) -> int:
+    return int(lib().mesa_qkv_norm_rope_bwd_q_workspace_bytes(heads, int(dtype)))
+
+
+def attention_fwd_workspace_bytes(a: Attention, dtype: int = F16) -> int:
+    return int(lib().mesa_attention_fwd_workspace_bytes(a, int(dtype)))
+
+
+def attention_bwd_q_workspace_bytes(a: Attention, q_codes=True, k_codes=True, v_codes=True, dtype: int = F16) -> int:
+    return int(lib().mesa_attention_bwd_q_workspace_bytes(a, int(bool(q_codes)), int(bool(k_codes)), int(bool(v_codes)), int(dtype)))
+
+
+def _here(t):
+    """a tensor of the current device, whose stream the call goes to"""
+    if not t.is_cuda:
+        raise ValueError("libmesa takes device tensors only")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError("the tensors have to be on the current device")
+
+
+def _flat(t, dtype, count, what):
+    """a contiguous tensor of so many elements at least, or None"""
+    if t is None:
+        return None
+    _here(t)
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() < count:
+        raise ValueError(f"{what}: a contiguous {dtype} tensor of {count} elements is wanted")
+    return t.data_ptr()
+
+
+def _rows(t, dtype, rows, width, what):
+    """(rows, at least width) with elements side by side: its address and row stride"""
+    _here(t)
+    if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] < width or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: a ({rows}, {width} or more) {dtype} tensor with elements side by side is wanted")
+    return t.data_ptr(), (t.stride(0) if rows > 1 else max(8, (t.shape[1] + 7) // 8 * 8))
+
+
+def _qkv(heads, dtype, gamma_q, gamma_k, freq, pos, alpha, beta, rstd, every=True):
+    n = heads.Hq + heads.Hk
+    h = n + heads.Hv
+    return (_flat(gamma_q, dtype, heads.D, "gamma_q"), _flat(gamma_k, dtype, heads.D, "gamma_k"), _flat(freq, torch.float32, heads.rot // 2, "freq"),
+            _flat(pos, torch.int32, heads.axes * heads.T, "pos"), _flat(alpha, torch.float32, h, "alpha"), _flat(beta, torch.float32, h, "beta"),
+            _flat(rstd, torch.float32, heads.T * n, "rstd"))
+
+
+def mesa_qkv_norm_rope_fwd_q(x, heads: QkvHeads, gamma_q, gamma_k, freq, pos, alpha, beta, lam, y, rstd, q, ws, mode=ROUND_STOCHASTIC, seed=0, offset=0):
+    """x (T, (Hq+Hk+Hv)*D or more) may be a slice of wider rows; y (T, Hq+Hk, D), q (T, Hq+Hk+Hv, D)"""
+    n = heads.Hq + heads.Hk
+    h = n + heads.Hv
+    dt = _dt(x)
+    px, row = _rows(x, x.dtype, heads.T, h * heads.D, "x")
+    gq, gk, fr, ps, al, be, rs = _qkv(heads, x.dtype, gamma_q, gamma_k, freq, pos, alpha, beta, rstd)
+    p, size = _ws_args(ws)
+    _check(lib().mesa_qkv_norm_rope_fwd_q(px, row, heads, gq, gk, fr, ps, al, be, float(lam), _flat(y, x.dtype, heads.T * n * heads.D, "y"), rs,
+                                          _flat(q, torch.int8, heads.T * h * heads.D, "q"), int(mode), int(seed), int(offset), p, size, dt, _stream()),
+           "mesa_qkv_norm_rope_fwd_q")
+
+
+def mesa_qkv_norm_rope_recompute_q(q, heads: QkvHeads, gamma_q, gamma_k, freq, pos, alpha, beta, rstd, y):
+    n = heads.Hq + heads.Hk
+    dt = _dt(y)
+    gq, gk, fr, ps, al, be, rs = _qkv(heads, y.dtype, gamma_q, gamma_k, freq, pos, alpha, beta, rstd)
+    _check(lib().mesa_qkv_norm_rope_recompute_q(_flat(q, torch.int8, heads.T * (n + heads.Hv) * heads.D, "q"), heads, gq, gk, fr, ps, al, be, rs,
+                                                _flat(y, y.dtype, heads.T * n * heads.D, "y"), dt, _stream()), "mesa_qkv_norm_rope_recompute_q")
+
+
+def mesa_qkv_norm_rope_bwd_q(q, heads: QkvHeads, gamma_q, gamma_k, freq, pos, alpha, beta, rstd, dy, dx, dgamma_q, dgamma_k, ws):
+    """dy (T, Hq+Hk, D); dx (T, Hq+Hk, D) or (T, (Hq+Hk)*D or more), a slice of wider rows: what lies beyond the Hq+Hk heads stays as it is"""
+    n = heads.Hq + heads.Hk
+    dt = _dt(dy)
+    if dx.dim() == 3 and dx.is_contiguous():
+        dx = dx.view(dx.shape[0], -1)
+    pdx, row = _rows(dx, dy.dtype, heads.T, n * heads.D, "dx")
+    gq, gk, fr, ps, al, be, rs = _qkv(heads, dy.dtype, gamma_q, gamma_k, freq, pos, alpha, beta, rstd)
+    p, size = _ws_args(ws)
+    _check(lib().mesa_qkv_norm_rope_bwd_q(_flat(q, torch.int8, heads.T * (n + heads.Hv) * heads.D, "q"), heads, gq, gk, fr, ps, al, be, rs,
+                                          _flat(dy, dy.dtype, heads.T * n * heads.D, "dy"), pdx, row, _flat(dgamma_q, torch.float32, heads.D, "dgamma_q"),
+                                          _flat(dgamma_k, torch.float32, heads.D, "dgamma_k"), p, size, dt, _stream()), "mesa_qkv_norm_rope_bwd_q")
+
+
+def mesa_attention_bounds(lo, hi, Nk, causal, window=0, kv_len=None, q_start=None, prefix=None, doc=None):
+    """lo, hi (B, Nq) int32; kv_len, q_start, prefix [B], doc (B, Nk) int32"""
+    if lo.dim() != 2 or lo.shape != hi.shape:
+        raise ValueError("lo and hi are (B, Nq)")
+    B, Nq = lo.shape
+    i32 = torch.int32
+    _check(lib().mesa_attention_bounds(_flat(lo, i32, B * Nq, "lo"), _flat(hi, i32, B * Nq, "hi"), B, Nq, int(Nk), int(bool(causal)), int(window),
+                                       _flat(kv_len, i32, B, "kv_len"), _flat(q_start, i32, B, "q_start"), _flat(prefix, i32, B, "prefix"),
+                                       _flat(doc, i32, B * int(Nk), "doc"), _stream()), "mesa_attention_bounds")
+
+
+def _strides(t, shape, dtype, what):
+    _here(t)
+    if t.dtype != dtype or tuple(t.shape) != shape or (shape[3] > 1 and t.stride(3) != 1):
+        raise ValueError(f"{what}: a {shape} {dtype} tensor with a head's elements side by side is wanted")
+    return (t.data_ptr(), *(0 if n <= 1 else st for n, st in zip(shape[:3], t.stride()[:3])))
+
+
+def _operand(x, shape, dtype, what):
+    """a tensor of the storage type, or (codes, alpha, beta)"""
+    if torch.is_tensor(x):
+        return AttentionIn(*_strides(x, shape, dtype, what), None, None)
+    codes, alpha, beta = x
+    return AttentionIn(*_strides(codes, shape, torch.int8, what), _flat(alpha, torch.float32, shape[2], what + ": alpha"), _flat(beta, torch.float32, shape[2], what + ": beta"))
+
+
+def _mask(a, lo, hi, slopes, q_start):
+    return AttentionMask(_flat(lo, torch.int32, a.B * a.Nq, "lo"), _flat(hi, torch.int32, a.B * a.Nq, "hi"), _flat(slopes, torch.float32, a.Hq, "slopes"),
+                         _flat(q_start, torch.int32, a.B, "q_start"))
+
+
+def mesa_attention_fwd(a: Attention, q, k, v, o, lse, ws=None, lo=None, hi=None, slopes=None, q_start=None):
+    """q, o (B, Nq, Hq, D), k, v (B, Nk, Hk, D), any strides that are multiples of 8 with a head's elements side by side; lse (B, Hq, Nq)"""
+    dt, d = _dt(q), q.dtype
+    rows, keys = (a.B, a.Nq, a.Hq, a.D), (a.B, a.Nk, a.Hk, a.D)
+    p, size = _ws_args(ws)
+    _check(lib().mesa_attention_fwd(a, _operand(q, rows, d, "q"), _operand(k, keys, d, "k"), _operand(v, keys, d, "v"), AttentionOut(*_strides(o, rows, d, "o")),
+                                    _flat(lse, torch.float32, a.B * a.Hq * a.Nq, "lse"), _mask(a, lo, hi, slopes, q_start), p, size, dt, _stream()), "mesa_attention_fwd")
+
+
+def mesa_attention_bwd_q(a: Attention, q, k, v, o, lse, do, dq, dk, dv, ws, lo=None, hi=None, slopes=None, q_start=None):
+    """q, k, v: tensors of the storage type, or (codes, alpha, beta) each; shapes and strides as for the forward"""
+    dt, d = _dt(do), do.dtype
+    rows, keys = (a.B, a.Nq, a.Hq, a.D), (a.B, a.Nk, a.Hk, a.D)
+    p, size = _ws_args(ws)
+    _check(lib().mesa_attention_bwd_q(a, _operand(q, rows, d, "q"), _operand(k, keys, d, "k"), _operand(v, keys, d, "v"), _operand(o, rows, d, "o"),
+                                      _flat(lse, torch.float32, a.B * a.Hq * a.Nq, "lse"), _operand(do, rows, d, "do"), AttentionOut(*_strides(dq, rows, d, "dq")),
+                                      AttentionOut(*_strides(dk, keys, d, "dk")), AttentionOut(*_strides(dv, keys, d, "dv")), _mask(a, lo, hi, slopes, q_start), p, size, dt,
+                                      _stream()), "mesa_attention_bwd_q")
 
 
 def mesa_stream_copy(src, dst, nbytes):

@@ -15,7 +15,8 @@ INCLUDE = PKG.parent / "include"
 LIB = PKG / "libmesa.so"
 FAST = PKG / ("_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 OBJ = PKG / "_build"
-SOURCES = ["stream_kernels.hip", "softmax_fwd.hip", "softmax_bwd.hip", "layernorm_fwd.hip", "layernorm_bwd.hip", "linear_dw.hip", "attn_matmul_bwd.hip", "lowbit.hip", "conv_dw.hip", "mfma_probe.hip"]
+SOURCES = ["stream_kernels.hip", "softmax_fwd.hip", "softmax_bwd.hip", "layernorm_fwd.hip", "layernorm_bwd.hip", "linear_dw.hip", "attn_matmul_bwd.hip", "lowbit.hip", "conv_dw.hip", "mfma_probe.hip", "qkv_norm_rope.hip",
+           "attention_fwd.hip", "attention_bwd.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 # -ffp-contract=off: no implicit fused multiply-adds anywhere; kernels that may fuse call fmaf.

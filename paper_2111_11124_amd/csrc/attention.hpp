@@ -1,0 +1,240 @@
+// attention.hpp -- what the attention kernels share: tiles of rows in LDS, matrix-core operands from them, scores.
+//
+// Every product is formed "transposed", with the rows a wave owns (queries in the forward and for dQ, keys for dK and dV) as the
+// COLUMNS of 32x32x16 MFMAs: a lane then holds one column, so that maxima, sums, log-sum-exps and masks of a row are one
+// value per lane, and a result tile, rounded to 16 bits, is in place as the B operand of the next product -- if the
+// contracted index is counted in the order in which the accumulator has it:
+//   accumulator register i of lane l:  row 8*(i/4) + 4*(l/32) + i%4,  column l%32
+//   B operand element e of lane l, registers 8g..8g+7 packed:  index 16g + 8*(e/4) + 4*(l/32) + e%4
+// and the A operand of that product is read from LDS in the same order: two transposing reads of four rows each, at
+// rows 16g + 4*(l/32) and 8 further on.
+//
+// A tile's rows are DP elements (DP: head_dim padded to 64 or 128 with zeros), in pieces of 16 bytes, piece c of row r
+// at place c ^ turn(r): eight consecutive rows' pieces c lie in eight different bank groups (plain reads), and four
+// consecutive rows' 32-byte pairs of pieces in four (transposing reads).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "api_util.hpp"
+#include "common.hpp"
+
+namespace mesa {
+
+typedef float at_acc __attribute__((ext_vector_type(16)));
+typedef __bf16 at_v8b __attribute__((ext_vector_type(8)));
+typedef _Float16 at_v8h __attribute__((ext_vector_type(8)));
+typedef short at_v4s __attribute__((ext_vector_type(4)));
+typedef __bf16 at_v2b __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr float kAtLow = -3.0e38f;      // a running maximum before anything is seen; finite, so that (-inf) - it is -inf
+constexpr int kAtDrop = 8;              // binary16 probabilities of the backward carry this power of two, clear of subnormal values
+
+template <typename T> struct AtNum;
+template <> struct AtNum<_Float16> {
+    static constexpr bool kHalf = true;
+    __device__ static __forceinline__ at_acc mfma(u32x4 a, u32x4 b, at_acc c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(at_v8h, a), __builtin_bit_cast(at_v8h, b), c, 0, 0, 0);
+    }
+    __device__ static __forceinline__ uint32_t pack(float a, float b)      // round to nearest even
+    {
+        h2 p;
+        p.x = _Float16(a);
+        p.y = _Float16(b);
+        return as_u32(p);
+    }
+};
+template <> struct AtNum<__bf16> {
+    static constexpr bool kHalf = false;
+    __device__ static __forceinline__ at_acc mfma(u32x4 a, u32x4 b, at_acc c)
+    {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(at_v8b, a), __builtin_bit_cast(at_v8b, b), c, 0, 0, 0);
+    }
+    __device__ static __forceinline__ uint32_t pack(float a, float b)
+    {
+        at_v2b p;
+        p.x = __bf16(a);
+        p.y = __bf16(b);
+        return __builtin_bit_cast(uint32_t, p);
+    }
+};
+
+// a tensor (B, tokens, heads, D) as the kernels see it; strides in bytes
+struct AtView {
+    const char *p;
+    int64_t batch, token, head;
+};
+struct AtOut {
+    char *p;
+    int64_t batch, token, head;
+};
+
+// the shape: rows of a (sequence, key head) pair are its tokens times the G query heads of the group, token by token
+struct AtShape {
+    int32_t B, Nq, Nk, Hq, Hk, G, D;
+    uint32_t R;                         // Nq * G
+    FastDiv div_g;
+    float c;                            // scores to powers of two: scale * log2(e); with a cap 2 log2(e) scale / cap
+    float cap2;                         // cap * log2(e)
+    float scale;
+    const int32_t *lo, *hi, *q_start;
+    const float *slopes;
+};
+
+struct AtRow {
+    uint32_t token, g;
+};
+__device__ __forceinline__ AtRow at_row(const AtShape &s, uint32_t r)
+{
+    AtRow w;
+    w.token = s.G == 1 ? r : fastdiv(r, s.div_g);
+    w.g = r - w.token * uint32_t(s.G);
+    return w;
+}
+// the interval of row `token` of sequence b, cut to the keys that there are; 0, 0 where it holds none
+__device__ __forceinline__ void at_interval(const AtShape &s, int b, uint32_t token, int &lo, int &hi)
+{
+    lo = 0;
+    hi = s.Nk;
+    if (s.lo) {
+        lo = s.lo[int64_t(b) * s.Nq + token];
+        hi = s.hi[int64_t(b) * s.Nq + token];
+        lo = lo < 0 ? 0 : lo;
+        hi = hi > s.Nk ? s.Nk : hi;
+    }
+    if (lo >= hi) lo = hi = 0;
+}
+__device__ __forceinline__ int at_place(const AtShape &s, int b, uint32_t token)
+{
+    return int(token + uint32_t(s.q_start ? s.q_start[b] : s.Nk - s.Nq));
+}
+
+__device__ __forceinline__ int at_turn(int row) { return ((row & 3) << 1) ^ ((row >> 2) & 1); }
+
+// ROWS x DP elements from memory to LDS by NT threads, by way of registers.  Rows past `rows` and pieces past D become zeros.
+// `at(row)`: byte offset of a row from `base`.
+template <int NT, int ROWS, int DP> struct AtTile {
+    static constexpr int kPieces = DP / 8, kN = ROWS * kPieces / NT, kBytes = ROWS * DP * 2;
+    static_assert(ROWS * kPieces % NT == 0, "whole pieces per thread");
+    u32x4 r[kN];
+    template <typename At> __device__ __forceinline__ void load(const char *base, int rows, int D, At at)
+    {
+        const Span s(base, kNowhere);
+#pragma unroll
+        for (int k = 0; k < kN; ++k) {
+            const int i = int(threadIdx.x) + k * NT, row = i / kPieces, piece = i % kPieces;
+            s.load_kept(row < rows && piece * 8 < D ? uint32_t(at(row)) + piece * 16 : kNowhere, r[k]);
+        }
+    }
+    __device__ __forceinline__ void store(char *lds) const
+    {
+#pragma unroll
+        for (int k = 0; k < kN; ++k) {
+            const int i = int(threadIdx.x) + k * NT, row = i / kPieces, piece = i % kPieces;
+            *reinterpret_cast<u32x4 *>(lds + row * (DP * 2) + ((piece ^ at_turn(row)) << 4)) = r[k];
+        }
+    }
+};
+
+// A operand, rows as they lie: rows row0..row0+31 of the tile, elements 16*ks ..+15
+template <int DP> __device__ __forceinline__ u32x4 at_plain(const char *lds, int row0, int ks, int lane)
+{
+    const int row = row0 + (lane & 31), piece = ks * 2 + (lane >> 5);
+    return *reinterpret_cast<const u32x4 *>(lds + row * (DP * 2) + ((piece ^ at_turn(lane & 31)) << 4));
+}
+// A operand, transposed: elements d0..d0+31 as its rows, the tile's rows row0..row0+15 as the contracted index
+template <int DP> __device__ __forceinline__ u32x4 at_transposed(const char *lds, int row0, int d0, int lane)
+{
+    const int sl = lane & 15, h = lane >> 5;
+    const int row = row0 + 4 * h + (sl >> 2), col = d0 + ((lane >> 4) & 1) * 16 + (sl & 3) * 4;
+    const char *p = lds + row * (DP * 2) + (((col >> 3) ^ at_turn(4 * h + (sl >> 2))) << 4) + (col & 7) * 2;
+    typedef __attribute__((address_space(3))) at_v4s *lds_v4s;
+    const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)p));
+    const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(p + 8 * DP * 2)));
+    return u32x4{a[0], a[1], b[0], b[1]};
+}
+
+// B operand straight from memory: elements 16*ks + 8*(lane/32) ..+7 of the lane's row, zeros past D
+__device__ __forceinline__ u32x4 at_column(const char *row, int ks, int lane, int D)
+{
+    const int d = ks * 16 + (lane >> 5) * 8;
+    return d < D ? *reinterpret_cast<const u32x4 *>(row + d * 2) : u32x4{0u, 0u, 0u, 0u};
+}
+
+// the partner's value of the same column (lane ^ 32) beside the lane's own
+__device__ __forceinline__ float at_pair_max(float v)
+{
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float at_pair_sum(float v)
+{
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+__device__ __forceinline__ int at_wave_min(int v)      // over the 32 columns; uniform
+{
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) { const int o = __shfl_xor(v, m, 64); v = o < v ? o : v; }
+    return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int at_wave_max(int v)
+{
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) { const int o = __shfl_xor(v, m, 64); v = o > v ? o : v; }
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
+__device__ __forceinline__ float at_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// tanh of x, for u = 2 log2(e) x:  1 - 2 / (2^u + 1); off by some 1e-7 in absolute value, as is the score by 1e-7 caps
+__device__ __forceinline__ float at_tanh(float u) { return fmaf(-2.0f, __builtin_amdgcn_rcpf(at_exp2(u) + 1.0f), 1.0f); }
+
+// index within a 32-row accumulator tile of register i, without the lane's part 4*(lane/32)
+__device__ __forceinline__ constexpr int at_reg_row(int i) { return 8 * (i / 4) + i % 4; }
+
+// Eight accumulator registers' worth of "some column of this wave's sees it": bits as AND masks for the A operand of the product
+// that contracts this index, so that what no column sees (padding; infinities and NaN there) enters as zero and
+// not as 0 * NaN.  vis[e]: this lane's column sees index e of its half.
+__device__ __forceinline__ u32x4 at_seen(const bool vis[8], int lane)
+{
+    u32x4 m;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        uint32_t word = 0u;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint64_t any = __ballot(vis[2 * w + k]);
+            const bool seen = lane < 32 ? uint32_t(any) != 0u : uint32_t(any >> 32) != 0u;
+            word |= seen ? (k ? 0xFFFF0000u : 0x0000FFFFu) : 0u;
+        }
+        m[w] = word;
+    }
+    return m;
+}
+
+// four consecutive elements of a result row
+template <typename T> __device__ __forceinline__ void at_store4(char *p, float a, float b, float c, float d)
+{
+    *reinterpret_cast<u32x2 *>(p) = u32x2{AtNum<T>::pack(a, b), AtNum<T>::pack(c, d)};
+}
+
+// ---- host side ----
+inline bool at_valid(const mesa_attention &a)
+{
+    const int64_t top = int64_t(1) << 30;
+    return a.B >= 0 && a.Nq >= 0 && a.Nk >= 0 && a.Hk >= 1 && a.Hq >= 1 && a.Hq % a.Hk == 0 && a.D >= 1 && a.scale > 0.0f && a.scale < __builtin_inff() && a.cap >= 0.0f &&
+           a.cap < __builtin_inff() && a.B < top && a.Nq < top && a.Nk < top && a.Hq < top && a.Hk < top;
+}
+// MESA_OK, or why the kernels do not take this shape
+inline mesa_status at_supported(const mesa_attention &a, mesa_dtype dt)
+{
+    if (!valid_dtype(dt) || !at_valid(a)) return MESA_ERR_INVALID_ARG;
+    if (dt == MESA_F32 || a.D % 8 != 0 || a.D > 128) return MESA_ERR_UNSUPPORTED;
+    if (a.Nq * (a.Hq / a.Hk) >= (int64_t(1) << 31)) return MESA_ERR_UNSUPPORTED;
+    return MESA_OK;
+}
+AtShape at_shape(const mesa_attention &a, const mesa_attention_mask &m);
+
+}  // namespace mesa

@@ -1,0 +1,754 @@
+// attention_bwd.hip -- the backward of attention over intervals of keys, at operands that were saved as codes.
+//   p = exp(s - lse),  delta_i = do_i.o_i,  ds = p (do.v - delta) (times the cap's derivative 1 - tanh^2)
+//   dv_j = sum_i p_ij do_i,   dk_j = scale sum_i ds_ij q_i,   dq_i = scale sum_j ds_ij k_j
+//
+// Four steps on the stream: codes become 16-bit operands in the workspace (they are read many times over); a pass over
+// the rows leaves delta, log-sum-exps and intervals, row by row; then keys (dk and dv: a wave owns 32 keys and walks over
+// the rows) and queries (dq: a wave owns 32 rows and walks over the keys).  The scores are formed in both, seven products instead
+// of five: dq added up across workgroups would need atomics, whose order changes the result.  A group's heads are rows of
+// the same walk, so the gradients of a shared key head add up in registers.
+//
+// binary16 storage: p goes into its products 2^8-fold, and ds with a power of two from the norms of do and v that keeps it
+// below 2^15 and as far as it can from the subnormal values, where products of long rows' probabilities and of small
+// gradients would lose their bits.  bfloat16 has the exponents of binary32 and needs neither.
+#include "attention.hpp"
+
+namespace mesa {
+
+bool at_strides(const mesa_attention &a, int64_t tokens, int64_t heads, int64_t batch, int64_t token, int64_t head);
+
+constexpr int kAbRows = 128;           // rows of a workgroup of the row pass, and keys of one of its value norms
+constexpr int kAbTile = 32;            // rows per step of the walk over rows
+constexpr int kAbKeys = 128;           // keys of a workgroup
+
+struct AbRows {                        // what the row pass leaves, [b * Hk + key head][padded rows]
+    float *lse2, *delta;               // log-sum-exp in powers of two; padded rows and rows that see nothing: 3e38, 0
+    int32_t *lo, *hi;                  // padded rows: 0, 0
+    int4 *tiles;                       // [..][tile]: least lo, largest hi of the rows that see something; largest lo, least hi of all
+    float2 *most;                      // [..][row block]: largest |do|, largest |delta|    (binary16 only)
+    float *values;                     // [..][128 keys]: largest |v|                       (binary16 only)
+    uint32_t rows, blocks, key_blocks; // padded rows (a multiple of 128), row blocks, blocks of 128 keys
+};
+struct AtBwd {
+    AtShape s;
+    AtView q, k, v, o, dO;
+    AtOut dq, dk, dv;
+    const float *lse;
+    AbRows w;
+    float *part;                       // [split][b * Hk + head][Nk][2][D]; null: no split
+    uint32_t heads, key_blocks, splits, row_blocks;
+};
+
+// codes to contiguous (B, heads, tokens, D) elements, as mesa_dequantize; eight per thread
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_attn_operand(AtView q, const float *__restrict__ alpha, const float *__restrict__ beta, char *__restrict__ out, int heads, int tokens,
+                                                           int D, int64_t pieces)
+{
+    const int64_t id = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+    if (id >= pieces) return;
+    const int per = D / 8;
+    const int64_t row = id / per, bh = row / tokens, b = bh / heads;
+    const int e = int(id - row * per) * 8, t = int(row - bh * tokens), h = int(bh - b * heads);
+    const u32x2 c = *reinterpret_cast<const u32x2 *>(q.p + b * q.batch + int64_t(t) * q.token + int64_t(h) * q.head + e);
+    float f[8];
+    codes_to_float(c, f);
+    const float s = alpha[h] / 255.0f, z = beta[h];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float y = f[k] * s;
+        f[k] = y + z;
+    }
+    Store<T>::store(out, row * D + e, Store<T>::pack(f));
+}
+
+// The row pass.  Workgroups [0, blocks) of a head: 128 rows' deltas, log-sum-exps, intervals and the summaries of their four
+// tiles; further ones (binary16): the largest norm of 128 keys' values.  Eight or sixteen lanes per row.
+template <typename T, int DP>
+__global__ __launch_bounds__(kThreads) void k_attn_rows(const AtBwd a)
+{
+    constexpr int kLanes = DP / 8, kPer = kThreads / kLanes;
+    const AtShape &s = a.s;
+    const uint32_t head = blockIdx.x % a.heads, blk = blockIdx.x / a.heads;
+    const int b = int(head / uint32_t(s.Hk)), hk = int(head) - b * s.Hk;
+    const int tid = threadIdx.x, part = tid % kLanes, first = tid / kLanes;
+    __shared__ float top[2][kThreads / 64];
+    float most = 0.0f, most_delta = 0.0f;
+    if (blk >= a.w.blocks) {                               // values
+        const uint32_t kb = blk - a.w.blocks;
+        for (int r = first; r < kAbRows; r += kPer) {
+            const int j = int(kb) * kAbRows + r;
+            float ss = 0.0f;
+            if (j < s.Nk && part * 8 < s.D) {
+                float f[8];
+                Store<T>::unpack(Store<T>::load(a.v.p + int64_t(b) * a.v.batch + int64_t(j) * a.v.token + int64_t(hk) * a.v.head, part * 8), f);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) ss = fmaf(f[k], f[k], ss);
+            }
+            ss = lanes_sum_dpp<kLanes>(ss);
+            if (ss < __builtin_inff()) most = fmaxf(most, ss);   // not finite: a row that no query sees
+        }
+    } else {
+        __shared__ uint32_t empty[kAbRows / 32];
+        if (tid < kAbRows) {
+            const uint32_t r = blk * kAbRows + tid;
+            int lo = 0, hi = 0;
+            float lse2 = 3.0e38f;
+            if (r < s.R) {
+                const AtRow row = at_row(s, r);
+                at_interval(s, b, row.token, lo, hi);
+                if (hi > 0) {
+                    lse2 = a.lse[(int64_t(b) * s.Hq + hk * s.G + int(row.g)) * s.Nq + row.token] * kLog2e;
+                    if (AtNum<T>::kHalf) lse2 -= float(kAtDrop);
+                }
+            }
+            const int64_t at = int64_t(head) * a.w.rows + r;
+            a.w.lse2[at] = lse2;
+            a.w.lo[at] = lo;
+            a.w.hi[at] = hi;
+            const uint64_t none = __ballot(hi == 0);
+            int l0 = hi > 0 ? lo : 0x7FFFFFFF, h1 = hi, l1 = lo, h0 = hi;
+#pragma unroll
+            for (int m = 1; m < 32; m <<= 1) {
+                int x = __shfl_xor(l0, m, 64); l0 = x < l0 ? x : l0;
+                x = __shfl_xor(h1, m, 64); h1 = x > h1 ? x : h1;
+                x = __shfl_xor(l1, m, 64); l1 = x > l1 ? x : l1;
+                x = __shfl_xor(h0, m, 64); h0 = x < h0 ? x : h0;
+            }
+            if ((tid & 31) == 0) {
+                a.w.tiles[(int64_t(head) * a.w.rows + r) / 32] = make_int4(l0, h1, l1, h0);
+                empty[tid >> 5] = uint32_t(none >> (tid & 32));
+            }
+        }
+        __syncthreads();
+        for (int x = first; x < kAbRows; x += kPer) {
+            const uint32_t r = blk * kAbRows + x;
+            const bool live = r < s.R && !(empty[x >> 5] >> (x & 31) & 1u);
+            float dot = 0.0f, ss = 0.0f;
+            if (live && part * 8 < s.D) {
+                const AtRow row = at_row(s, r);
+                const int64_t h = hk * s.G + int64_t(row.g);
+                float f[8], g[8];
+                Store<T>::unpack(Store<T>::load(a.o.p + int64_t(b) * a.o.batch + int64_t(row.token) * a.o.token + h * a.o.head, part * 8), f);
+                Store<T>::unpack(Store<T>::load(a.dO.p + int64_t(b) * a.dO.batch + int64_t(row.token) * a.dO.token + h * a.dO.head, part * 8), g);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    dot = fmaf(f[k], g[k], dot);
+                    ss = fmaf(g[k], g[k], ss);
+                }
+            }
+            dot = lanes_sum_dpp<kLanes>(dot);
+            if (part == 0) a.w.delta[int64_t(head) * a.w.rows + r] = dot;
+            if (AtNum<T>::kHalf) {
+                most = fmaxf(most, lanes_sum_dpp<kLanes>(ss));
+                most_delta = fmaxf(most_delta, fabsf(dot));
+            }
+        }
+    }
+    if (!AtNum<T>::kHalf) return;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        most = fmaxf(most, __shfl_xor(most, m, 64));
+        most_delta = fmaxf(most_delta, __shfl_xor(most_delta, m, 64));
+    }
+    if ((tid & 63) == 0) {
+        top[0][tid >> 6] = most;
+        top[1][tid >> 6] = most_delta;
+    }
+    __syncthreads();
+    if (tid == 0) {
+        for (int w = 1; w < kThreads / 64; ++w) {
+            most = fmaxf(most, top[0][w]);
+            most_delta = fmaxf(most_delta, top[1][w]);
+        }
+        if (blk >= a.w.blocks) a.w.values[int64_t(head) * a.w.key_blocks + (blk - a.w.blocks)] = sqrtf(most);
+        else a.w.most[int64_t(head) * a.w.blocks + blk] = make_float2(sqrtf(most), most_delta);
+    }
+}
+
+// the exponent e with 2^e * bound within [2^13, 2^14): |ds| stays below 2^15 with a bound on |do.v| + |delta|, rounding included
+__device__ __forceinline__ int ab_exponent(float bound)
+{
+    if (!(bound > 0.0f)) return 0;
+    const int e = 13 - (int(__float_as_uint(bound) >> 23) - 127);
+    return e < -60 ? -60 : e > 100 ? 100 : e;
+}
+__device__ __forceinline__ float ab_pow2(int e) { return __uint_as_float(uint32_t(127 + e) << 23); }   // -126 <= e <= 127
+
+// scores of one accumulator in powers of two and, with a cap, the cap's derivative; away: place - key for register 0
+// ALONG: the registers count keys (a lane is a row), else rows (a lane is a key)
+template <bool CAP> __device__ __forceinline__ float ab_score(const AtShape &s, float x, float &slope)
+{
+    if (!CAP) return x * s.c;
+    const float t = at_tanh(x * s.c);
+    slope = fmaf(-t, t, 1.0f);
+    return s.cap2 * t;
+}
+
+// ---------------------------------------------------------------------------------------------
+// dq: a wave owns 32 rows
+// ---------------------------------------------------------------------------------------------
+template <typename T, int DP, int NW, int BN, bool CAP, bool BIAS>
+__global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
+{
+    typedef AtNum<T> Num;
+    typedef AtTile<NW * 64, BN, DP> Tile;
+    constexpr int kKs = DP / 16, kDt = DP / 32, kSub = BN / 32;
+    __shared__ __attribute__((aligned(16))) char lds[4 * Tile::kBytes];
+    __shared__ int range[2][NW];
+    const AtShape &s = a.s;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), half = lane >> 5;
+    const uint32_t head = blockIdx.x % a.heads, rb = a.row_blocks - 1 - blockIdx.x / a.heads;
+    const int b = int(head / uint32_t(s.Hk)), hk = int(head) - b * s.Hk;
+    const uint32_t r_own = (rb * NW + wave) * 32 + (lane & 31), r = r_own < s.R ? r_own : s.R - 1;
+    const AtRow row = at_row(s, r);
+    const int hq = hk * s.G + int(row.g);
+    const int64_t at = int64_t(head) * a.w.rows + r;
+    const int lo = a.w.lo[at], hi = a.w.hi[at];
+    const float lse2 = a.w.lse2[at], delta = a.w.delta[at];
+    const int wlo = at_wave_min(hi > 0 ? lo : 0x7FFFFFFF), whi = at_wave_max(hi), flo = at_wave_max(lo), fhi = at_wave_min(hi);
+    if (lane == 0) {
+        range[0][wave] = wlo;
+        range[1][wave] = whi;
+    }
+    u32x4 qf[kKs], gf[kKs];
+    {
+        const char *p = a.q.p + int64_t(b) * a.q.batch + int64_t(row.token) * a.q.token + int64_t(hq) * a.q.head;
+        const char *g = a.dO.p + int64_t(b) * a.dO.batch + int64_t(row.token) * a.dO.token + int64_t(hq) * a.dO.head;
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) {
+            qf[ks] = at_column(p, ks, lane, s.D);
+            gf[ks] = at_column(g, ks, lane, s.D);
+        }
+    }
+    const float slope2 = BIAS ? s.slopes[hq] * kLog2e : 0.0f;
+    const int place = BIAS ? at_place(s, b, row.token) : 0;
+    __syncthreads();
+    int blo = 0x7FFFFFFF, bhi = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        blo = range[0][w] < blo ? range[0][w] : blo;
+        bhi = range[1][w] > bhi ? range[1][w] : bhi;
+    }
+    const int t0 = __builtin_amdgcn_readfirstlane(bhi > 0 ? blo / BN : 0), t1 = __builtin_amdgcn_readfirstlane(bhi > 0 ? (bhi + BN - 1) / BN : 0);
+
+    float mul = 1.0f, undo = s.scale;                 // of ds, and of the sums
+    if (Num::kHalf) {
+        float ss = 0.0f, vmax = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) {
+            float f[8];
+            Store<T>::unpack(gf[ks], f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) ss = fmaf(f[k], f[k], ss);
+        }
+        ss = at_pair_sum(ss);
+        for (int kb = t0 * BN / kAbRows; kb * kAbRows < t1 * BN && kb < int(a.w.key_blocks); ++kb) vmax = fmaxf(vmax, a.w.values[int64_t(head) * a.w.key_blocks + kb]);
+        const int e = ab_exponent(sqrtf(ss) * vmax + fabsf(delta));
+        mul = ab_pow2(e - kAtDrop);
+        undo = s.scale * ab_pow2(-e);
+    }
+
+    const char *kbase = a.k.p + int64_t(b) * a.k.batch + int64_t(hk) * a.k.head, *vbase = a.v.p + int64_t(b) * a.v.batch + int64_t(hk) * a.v.head;
+    Tile tk, tv;
+    auto fetch = [&](int t) __attribute__((always_inline)) {
+        const int j0 = t * BN;
+        tk.load(kbase + int64_t(j0) * a.k.token, s.Nk - j0, s.D, [&](int x) { return x * int(a.k.token); });
+        tv.load(vbase + int64_t(j0) * a.v.token, s.Nk - j0, s.D, [&](int x) { return x * int(a.v.token); });
+    };
+    at_acc dq[kDt];
+#pragma unroll
+    for (int d = 0; d < kDt; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dq[d][i] = 0.0f;
+
+    auto work = [&](const char *lk, const char *lv, int j0, auto masked) __attribute__((always_inline)) {
+        constexpr bool kMasked = decltype(masked)::value;
+#pragma unroll
+        for (int t = 0; t < kSub; ++t) {
+            at_acc x, y;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = y[i] = 0.0f;
+#pragma unroll
+            for (int ks = 0; ks < kKs; ++ks) x = Num::mfma(at_plain<DP>(lk, t * 32, ks, lane), qf[ks], x);
+#pragma unroll
+            for (int ks = 0; ks < kKs; ++ks) y = Num::mfma(at_plain<DP>(lv, t * 32, ks, lane), gf[ks], y);
+            const int first = j0 + t * 32 + 4 * half;
+            const float away = BIAS ? float(place - first) : 0.0f;
+            u32x4 ds[2], seen[2];
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                bool vis[8];
+                float z[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int i = 8 * g + e;
+                    float slope = 1.0f, p;
+                    if (!CAP && !BIAS) {
+                        p = at_exp2(fmaf(x[i], s.c, -lse2));
+                    } else {
+                        float sc = ab_score<CAP>(s, x[i], slope);
+                        if (BIAS) sc = fmaf(-slope2, fabsf(away - float(at_reg_row(i))), sc);
+                        p = at_exp2(sc - lse2);
+                    }
+                    z[e] = p * (y[i] - delta);
+                    if (CAP) z[e] *= slope;
+                    if (Num::kHalf) z[e] *= mul;
+                    if (kMasked) {
+                        vis[e] = uint32_t(first + at_reg_row(i) - lo) < uint32_t(hi - lo);
+                        z[e] = vis[e] ? z[e] : 0.0f;
+                    }
+                }
+#pragma unroll
+                for (int w = 0; w < 4; ++w) ds[g][w] = Num::pack(z[2 * w], z[2 * w + 1]);
+                if (kMasked) seen[g] = at_seen(vis, lane);
+            }
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int d = 0; d < kDt; ++d) {
+                    u32x4 f = at_transposed<DP>(lk, t * 32 + g * 16, d * 32, lane);
+                    if (kMasked) f &= seen[g];
+                    dq[d] = Num::mfma(f, ds[g], dq[d]);
+                }
+        }
+    };
+    if (t0 < t1) fetch(t0);
+    for (int t = t0, cur = 0; t < t1; ++t, cur ^= 1) {
+        char *lk = lds + cur * 2 * Tile::kBytes, *lv = lk + Tile::kBytes;
+        tk.store(lk);
+        tv.store(lv);
+        __syncthreads();
+        if (t + 1 < t1) fetch(t + 1);
+        const int j0 = t * BN;
+        if (j0 + BN <= wlo || j0 >= whi) continue;
+        if (j0 >= flo && j0 + BN <= fhi) work(lk, lv, j0, std::false_type());
+        else work(lk, lv, j0, std::true_type());
+    }
+    if (r_own >= s.R) return;
+    char *p = a.dq.p + int64_t(b) * a.dq.batch + int64_t(row.token) * a.dq.token + int64_t(hq) * a.dq.head;
+#pragma unroll
+    for (int d = 0; d < kDt; ++d)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int e = d * 32 + 8 * w + 4 * half;
+            if (e < s.D) at_store4<T>(p + e * 2, dq[d][4 * w] * undo, dq[d][4 * w + 1] * undo, dq[d][4 * w + 2] * undo, dq[d][4 * w + 3] * undo);
+        }
+}
+
+// ---------------------------------------------------------------------------------------------
+// dk, dv: a wave owns 32 keys
+// ---------------------------------------------------------------------------------------------
+template <typename T, int DP, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd a)
+{
+    typedef AtNum<T> Num;
+    constexpr int kRows = kAbTile;
+    typedef AtTile<256, kRows, DP> Tile;
+    constexpr int kKs = DP / 16, kDt = DP / 32;
+    constexpr int kInfo = BIAS ? 6 : 4;               // lse2, delta, lo, hi and, with a bias, slope and place
+    __shared__ __attribute__((aligned(16))) char lds[4 * Tile::kBytes];
+    __shared__ __attribute__((aligned(16))) uint32_t info[2][kInfo][kRows];
+    const AtShape &s = a.s;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
+    const uint32_t head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, split = rest % a.splits, kb = rest / a.splits;   // the keys that most rows see first
+    const int b = int(head / uint32_t(s.Hk)), hk = int(head) - b * s.Hk;
+    const int k0 = int(kb) * kAbKeys, j_own = k0 + wave * 32 + (lane & 31), j = j_own < s.Nk ? j_own : s.Nk - 1;
+    u32x4 kf[kKs], vf[kKs];
+    {
+        const char *p = a.k.p + int64_t(b) * a.k.batch + int64_t(j) * a.k.token + int64_t(hk) * a.k.head;
+        const char *v = a.v.p + int64_t(b) * a.v.batch + int64_t(j) * a.v.token + int64_t(hk) * a.v.head;
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) {
+            kf[ks] = at_column(p, ks, lane, s.D);
+            vf[ks] = at_column(v, ks, lane, s.D);
+        }
+    }
+    float mul = 1.0f, undo = s.scale, undo_v = 1.0f;
+    if (Num::kHalf) {
+        float ss = 0.0f, most = 0.0f, most_delta = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) {
+            float f[8];
+            Store<T>::unpack(vf[ks], f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) ss = fmaf(f[k], f[k], ss);
+        }
+        ss = at_pair_sum(ss);
+        for (uint32_t k = lane; k < a.w.blocks; k += 64) {
+            const float2 m = a.w.most[int64_t(head) * a.w.blocks + k];
+            most = fmaxf(most, m.x);
+            most_delta = fmaxf(most_delta, m.y);
+        }
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            most = fmaxf(most, __shfl_xor(most, m, 64));
+            most_delta = fmaxf(most_delta, __shfl_xor(most_delta, m, 64));
+        }
+        const int e = ab_exponent(sqrtf(ss) * most + most_delta);
+        mul = ab_pow2(e - kAtDrop);
+        undo = s.scale * ab_pow2(-e);
+        undo_v = ab_pow2(-kAtDrop);
+    }
+    const char *qbase = a.q.p + int64_t(b) * a.q.batch + int64_t(hk) * s.G * a.q.head, *gbase = a.dO.p + int64_t(b) * a.dO.batch + int64_t(hk) * s.G * a.dO.head;
+    const int64_t info_at = int64_t(head) * a.w.rows;
+    const int4 *tiles = a.w.tiles + info_at / 32;
+    const int count = int((s.R + kRows - 1) / kRows);       // tiles of rows; this workgroup's: split, split + splits, ...
+    const int mine = (count - int(split) + int(a.splits) - 1) / int(a.splits);
+
+    // the next tile that this workgroup's keys meet: 64 summaries at a time, one per lane
+    int base = -64;
+    uint64_t meets = 0, whole = 0;
+    auto next = [&]() __attribute__((always_inline)) {
+        while (meets == 0) {
+            base += 64;
+            if (base >= mine) return -1;
+            const int n = base + lane;
+            bool in = false, all = false;
+            if (n < mine) {
+                const int4 t = tiles[int(split) + n * int(a.splits)];
+                in = t.y > k0 && t.x < k0 + kAbKeys;
+                all = t.w >= k0 + kAbKeys && t.z <= k0;
+            }
+            meets = __ballot(in);
+            whole = __ballot(all);
+        }
+        const int bit = __builtin_ctzll(meets);
+        meets &= meets - 1;
+        return ((int(split) + (base + bit) * int(a.splits)) << 1) | int(whole >> bit & 1u);
+    };
+    Tile tq, tg;
+    uint32_t word = 0;
+    auto fetch = [&](int t) __attribute__((always_inline)) {
+        const uint32_t r0 = uint32_t(t) * kRows;
+        const AtRow first = at_row(s, r0);
+        const int left = int(s.R - r0 < kRows ? s.R - r0 : kRows);
+        // a row's place from the first row's token
+        auto off = [&](int64_t token, int64_t headstep, int x) __attribute__((always_inline)) {
+            if (s.G == 1) return uint32_t(x * int(token));
+            const uint32_t u = first.g + uint32_t(x), n = fastdiv(u, s.div_g);
+            return n * uint32_t(token) + (u - n * uint32_t(s.G)) * uint32_t(headstep);
+        };
+        tq.load(qbase + int64_t(first.token) * a.q.token, left, s.D, [&](int x) { return off(a.q.token, a.q.head, x); });
+        tg.load(gbase + int64_t(first.token) * a.dO.token, left, s.D, [&](int x) { return off(a.dO.token, a.dO.head, x); });
+        if (tid < kInfo * kRows) {
+            const int what = tid / kRows, x = tid % kRows;
+            const int64_t at = info_at + r0 + x;
+            if (what == 0) word = __float_as_uint(a.w.lse2[at]);
+            else if (what == 1) word = __float_as_uint(a.w.delta[at]);
+            else if (what == 2) word = uint32_t(a.w.lo[at]);
+            else if (what == 3) word = uint32_t(a.w.hi[at]);
+            else if (BIAS) {
+                const AtRow row = at_row(s, r0 + x < s.R ? r0 + x : s.R - 1);
+                word = what == 4 ? __float_as_uint(s.slopes[hk * s.G + int(row.g)] * kLog2e) : uint32_t(at_place(s, b, row.token));
+            }
+        }
+    };
+    at_acc dk[kDt], dv[kDt];
+#pragma unroll
+    for (int d = 0; d < kDt; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dk[d][i] = dv[d][i] = 0.0f;
+
+    auto work = [&](const char *lq, const char *lg, const uint32_t (*in)[kRows], auto masked) __attribute__((always_inline)) {
+        constexpr bool kMasked = decltype(masked)::value;
+        at_acc x, y;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = y[i] = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) x = Num::mfma(at_plain<DP>(lq, 0, ks, lane), kf[ks], x);
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) y = Num::mfma(at_plain<DP>(lg, 0, ks, lane), vf[ks], y);
+        u32x4 p[2], ds[2], seen[2];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            bool vis[8];
+            float pe[8], z[8];
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const int at = 8 * (2 * g + w) + 4 * half;         // rows of four registers
+                const u32x4 l4 = *reinterpret_cast<const u32x4 *>(&in[0][at]), d4 = *reinterpret_cast<const u32x4 *>(&in[1][at]);
+                u32x4 lo4 = {}, hi4 = {}, sl4 = {}, pl4 = {};
+                if (kMasked) {
+                    lo4 = *reinterpret_cast<const u32x4 *>(&in[2][at]);
+                    hi4 = *reinterpret_cast<const u32x4 *>(&in[3][at]);
+                }
+                if (BIAS) {
+                    sl4 = *reinterpret_cast<const u32x4 *>(&in[kInfo - 2][at]);
+                    pl4 = *reinterpret_cast<const u32x4 *>(&in[kInfo - 1][at]);
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int e = 4 * w + c, i = 8 * g + e;
+                    const float lse2 = __uint_as_float(l4[c]);
+                    float slope = 1.0f;
+                    if (!CAP && !BIAS) {
+                        pe[e] = at_exp2(fmaf(x[i], s.c, -lse2));
+                    } else {
+                        float sc = ab_score<CAP>(s, x[i], slope);
+                        if (BIAS) sc = fmaf(-__uint_as_float(sl4[c]), fabsf(float(int(pl4[c]) - j_own)), sc);
+                        pe[e] = at_exp2(sc - lse2);
+                    }
+                    z[e] = pe[e] * (y[i] - __uint_as_float(d4[c]));
+                    if (CAP) z[e] *= slope;
+                    if (Num::kHalf) z[e] *= mul;
+                    if (kMasked) {
+                        vis[e] = j_own >= int(lo4[c]) && j_own < int(hi4[c]);
+                        pe[e] = vis[e] ? pe[e] : 0.0f;
+                        z[e] = vis[e] ? z[e] : 0.0f;
+                    }
+                }
+            }
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                p[g][w] = Num::pack(pe[2 * w], pe[2 * w + 1]);
+                ds[g][w] = Num::pack(z[2 * w], z[2 * w + 1]);
+            }
+            if (kMasked) seen[g] = at_seen(vis, lane);
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int d = 0; d < kDt; ++d) {
+                u32x4 f = at_transposed<DP>(lg, g * 16, d * 32, lane);
+                if (kMasked) f &= seen[g];
+                dv[d] = Num::mfma(f, p[g], dv[d]);
+                u32x4 h = at_transposed<DP>(lq, g * 16, d * 32, lane);
+                if (kMasked) h &= seen[g];
+                dk[d] = Num::mfma(h, ds[g], dk[d]);
+            }
+    };
+    int t = __builtin_amdgcn_readfirstlane(next());
+    if (t >= 0) fetch(t >> 1);
+    for (int cur = 0; t >= 0; cur ^= 1) {
+        char *lq = lds + cur * 2 * Tile::kBytes, *lg = lq + Tile::kBytes;
+        tq.store(lq);
+        tg.store(lg);
+        if (tid < kInfo * kRows) info[cur][tid / kRows][tid % kRows] = word;
+        __syncthreads();
+        const int after = __builtin_amdgcn_readfirstlane(next());
+        if (after >= 0) fetch(after >> 1);
+        if (t & 1) work(lq, lg, info[cur], std::false_type());
+        else work(lq, lg, info[cur], std::true_type());
+        t = after;
+    }
+    if (j_own >= s.Nk) return;
+    if (a.part) {
+        float *p = a.part + ((int64_t(split) * a.heads + head) * s.Nk + j_own) * 2 * s.D;
+#pragma unroll
+        for (int d = 0; d < kDt; ++d)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int e = d * 32 + 8 * w + 4 * half;
+                if (e < s.D) {
+                    *reinterpret_cast<float4 *>(p + e) = make_float4(dk[d][4 * w] * undo, dk[d][4 * w + 1] * undo, dk[d][4 * w + 2] * undo, dk[d][4 * w + 3] * undo);
+                    *reinterpret_cast<float4 *>(p + s.D + e) = make_float4(dv[d][4 * w] * undo_v, dv[d][4 * w + 1] * undo_v, dv[d][4 * w + 2] * undo_v, dv[d][4 * w + 3] * undo_v);
+                }
+            }
+        return;
+    }
+    char *pk = a.dk.p + int64_t(b) * a.dk.batch + int64_t(j_own) * a.dk.token + int64_t(hk) * a.dk.head;
+    char *pv = a.dv.p + int64_t(b) * a.dv.batch + int64_t(j_own) * a.dv.token + int64_t(hk) * a.dv.head;
+#pragma unroll
+    for (int d = 0; d < kDt; ++d)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int e = d * 32 + 8 * w + 4 * half;
+            if (e < s.D) {
+                at_store4<T>(pk + e * 2, dk[d][4 * w] * undo, dk[d][4 * w + 1] * undo, dk[d][4 * w + 2] * undo, dk[d][4 * w + 3] * undo);
+                at_store4<T>(pv + e * 2, dv[d][4 * w] * undo_v, dv[d][4 * w + 1] * undo_v, dv[d][4 * w + 2] * undo_v, dv[d][4 * w + 3] * undo_v);
+            }
+        }
+}
+
+// the splits added up in their order, four elements of dk or dv per thread
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_attn_add(const AtBwd a, int64_t pieces)
+{
+    const AtShape &s = a.s;
+    const int64_t id = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+    if (id >= pieces) return;
+    const int quads = s.D / 2;                              // of a key: D/4 of dk, D/4 of dv
+    const int64_t at = id / quads, head = at / s.Nk, step = int64_t(a.heads) * s.Nk * 2 * s.D;
+    const int x = int(id - at * quads), j = int(at - head * s.Nk);
+    const float *p = a.part + at * 2 * s.D + x * 4;
+    float4 v = *reinterpret_cast<const float4 *>(p);
+    for (uint32_t k = 1; k < a.splits; ++k) {
+        const float4 u = *reinterpret_cast<const float4 *>(p + k * step);
+        v.x += u.x;
+        v.y += u.y;
+        v.z += u.z;
+        v.w += u.w;
+    }
+    const int b = int(head) / s.Hk, hk = int(head) - b * s.Hk;
+    const bool key = x < s.D / 4;
+    const AtOut &o = key ? a.dk : a.dv;
+    at_store4<T>(o.p + int64_t(b) * o.batch + int64_t(j) * o.token + int64_t(hk) * o.head + (key ? x : x - s.D / 4) * 8, v.x, v.y, v.z, v.w);
+}
+
+// zeros: dq where there are no keys, dk and dv where there are no queries
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_attn_zero(AtOut o, int heads, int tokens, int D, int64_t pieces)
+{
+    const int64_t id = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+    if (id >= pieces) return;
+    const int per = D / 4;
+    const int64_t row = id / per, bt = row / heads, b = bt / tokens;
+    at_store4<T>(o.p + b * o.batch + (bt - b * tokens) * o.token + (row - bt * heads) * o.head + (id - row * per) * 8, 0.0f, 0.0f, 0.0f, 0.0f);
+}
+
+struct AtBwdPlan {
+    uint32_t rows, blocks, key_blocks, splits, row_blocks;
+    size_t info, part, operand[3], total;       // bytes
+};
+static size_t ab_up(size_t n) { return (n + 255) & ~size_t(255); }
+static AtBwdPlan at_bwd_plan(const mesa_attention &a, const bool codes[3])
+{
+    AtBwdPlan p;
+    const int64_t R = a.Nq * (a.Hq / a.Hk), heads = a.B * a.Hk;
+    p.blocks = uint32_t(ceil_div(R, kAbRows));
+    p.rows = p.blocks * kAbRows;
+    p.key_blocks = uint32_t(ceil_div(a.Nk, kAbKeys));
+    p.row_blocks = uint32_t(ceil_div(R, 128));
+    // few keys and long walks: the rows' tiles are dealt out to several workgroups and their sums added up
+    const int64_t have = heads * p.key_blocks, most = R / (8 * kAbTile);
+    int64_t n = have > 0 ? 512 / have : 1;
+    n = n > most ? most : n;
+    n = n > 32 ? 32 : n < 1 ? 1 : n;
+    p.splits = uint32_t(n);
+    const size_t h = size_t(heads);
+    p.info = ab_up(h * p.rows * 4) * 4 + ab_up(h * p.rows / 32 * sizeof(int4)) + ab_up(h * p.blocks * sizeof(float2)) + ab_up(h * p.key_blocks * sizeof(float));
+    p.part = n > 1 ? ab_up(size_t(n) * h * size_t(a.Nk) * 2 * size_t(a.D) * sizeof(float)) : 0;
+    const int64_t tokens[3] = {a.Nq, a.Nk, a.Nk}, hs[3] = {a.Hq, a.Hk, a.Hk};
+    p.total = p.info + p.part;
+    for (int k = 0; k < 3; ++k) {
+        p.operand[k] = codes[k] ? ab_up(size_t(a.B) * size_t(tokens[k]) * size_t(hs[k]) * size_t(a.D) * 2) : 0;
+        p.total += p.operand[k];
+    }
+    return p;
+}
+
+template <typename T, int DP, bool CAP, bool BIAS> static mesa_status at_bwd_launch(const AtBwd &a, hipStream_t s)
+{
+    hipLaunchKernelGGL((k_attn_dkv<T, DP, CAP, BIAS>), dim3(a.heads * a.key_blocks * a.splits), dim3(256), 0, s, a);
+    if (const mesa_status st = launch_status()) return st;
+    if (a.splits > 1) {
+        const int64_t pieces = int64_t(a.heads) * a.s.Nk * (a.s.D / 2);
+        hipLaunchKernelGGL(k_attn_add<T>, dim3(uint32_t(ceil_div(pieces, kThreads))), dim3(kThreads), 0, s, a, pieces);
+        if (const mesa_status st = launch_status()) return st;
+    }
+    hipLaunchKernelGGL((k_attn_dq<T, DP, 4, 32, CAP, BIAS>), dim3(a.heads * a.row_blocks), dim3(256), 0, s, a);
+    return launch_status();
+}
+template <typename T, int DP> static mesa_status at_bwd_forms(const AtBwd &a, bool cap, bool bias, hipStream_t s)
+{
+    hipLaunchKernelGGL((k_attn_rows<T, DP>), dim3(a.heads * (a.w.blocks + (AtNum<T>::kHalf ? a.w.key_blocks : 0))), dim3(kThreads), 0, s, a);
+    if (const mesa_status st = launch_status()) return st;
+    if (cap && bias) return at_bwd_launch<T, DP, true, true>(a, s);
+    if (cap) return at_bwd_launch<T, DP, true, false>(a, s);
+    if (bias) return at_bwd_launch<T, DP, false, true>(a, s);
+    return at_bwd_launch<T, DP, false, false>(a, s);
+}
+template <typename T> static mesa_status at_zero(const AtOut &o, int64_t B, int64_t tokens, int64_t heads, int64_t D, hipStream_t s)
+{
+    const int64_t pieces = B * tokens * heads * (D / 4);
+    if (pieces == 0) return MESA_OK;
+    hipLaunchKernelGGL(k_attn_zero<T>, dim3(uint32_t(ceil_div(pieces, kThreads))), dim3(kThreads), 0, s, o, int(heads), int(tokens), int(D), pieces);
+    return launch_status();
+}
+
+template <typename T>
+static mesa_status at_bwd(const mesa_attention &m, AtBwd &a, const AtBwdPlan &p, const mesa_attention_in *in, const bool codes[3], char *ws, bool bias, hipStream_t s)
+{
+    if (m.Nk == 0) return at_zero<T>(a.dq, m.B, m.Nq, m.Hq, m.D, s);
+    if (m.Nq == 0) {
+        if (const mesa_status st = at_zero<T>(a.dk, m.B, m.Nk, m.Hk, m.D, s)) return st;
+        return at_zero<T>(a.dv, m.B, m.Nk, m.Hk, m.D, s);
+    }
+    AtView *view[3] = {&a.q, &a.k, &a.v};
+    const int64_t tokens[3] = {m.Nq, m.Nk, m.Nk}, heads[3] = {m.Hq, m.Hk, m.Hk};
+    char *out = ws + p.info + p.part;
+    for (int k = 0; k < 3; ++k) {
+        if (!codes[k]) continue;
+        const int64_t pieces = m.B * tokens[k] * heads[k] * (m.D / 8);
+        const AtView c = {static_cast<const char *>(in[k].data), in[k].batch, in[k].token, in[k].head};
+        hipLaunchKernelGGL(k_attn_operand<T>, dim3(uint32_t(ceil_div(pieces, kThreads))), dim3(kThreads), 0, s, c, in[k].alpha, in[k].beta, out, int(heads[k]), int(tokens[k]),
+                           int(m.D), pieces);
+        if (const mesa_status st = launch_status()) return st;
+        *view[k] = AtView{out, heads[k] * tokens[k] * m.D * 2, m.D * 2, tokens[k] * m.D * 2};
+        out += p.operand[k];
+    }
+    return m.D <= 64 ? at_bwd_forms<T, 64>(a, m.cap > 0.0f, bias, s) : at_bwd_forms<T, 128>(a, m.cap > 0.0f, bias, s);
+}
+
+}  // namespace mesa
+
+using namespace mesa;
+
+extern "C" MESA_EXPORT size_t mesa_attention_bwd_q_workspace_bytes(mesa_attention a, int q_codes, int k_codes, int v_codes, mesa_dtype dt)
+{
+    const bool codes[3] = {q_codes != 0, k_codes != 0, v_codes != 0};
+    return at_supported(a, dt) == MESA_OK && a.B > 0 && a.Nq > 0 && a.Nk > 0 ? at_bwd_plan(a, codes).total : 0;
+}
+
+extern "C" MESA_EXPORT mesa_status mesa_attention_bwd_q(mesa_attention a, mesa_attention_in q, mesa_attention_in k, mesa_attention_in v, mesa_attention_in o, const float *lse,
+                                                        mesa_attention_in dO, mesa_attention_out dq, mesa_attention_out dk, mesa_attention_out dv, mesa_attention_mask m, void *ws,
+                                                        size_t ws_bytes, mesa_dtype dt, void *stream)
+{
+    if (const mesa_status st = at_supported(a, dt)) return st;
+    if (a.B == 0 || (a.Nq == 0 && a.Nk == 0)) return MESA_OK;
+    const mesa_attention_in in[3] = {q, k, v};
+    const int64_t tokens[3] = {a.Nq, a.Nk, a.Nk}, group = a.Hq / a.Hk;
+    bool codes[3];
+    for (int n = 0; n < 3; ++n) {
+        codes[n] = in[n].alpha != nullptr;
+        if (codes[n] != (in[n].beta != nullptr) || !aligned4(in[n].alpha) || !aligned4(in[n].beta)) return MESA_ERR_INVALID_ARG;
+        if (tokens[n] && !in[n].data) return MESA_ERR_INVALID_ARG;
+        if ((reinterpret_cast<uintptr_t>(in[n].data) & (codes[n] ? 7u : 15u)) != 0 || !at_strides(a, tokens[n], n == 0 ? group : 1, in[n].batch, in[n].token, in[n].head))
+            return MESA_ERR_INVALID_ARG;
+    }
+    if (a.Nq && (!o.data || !dO.data || !dq.data || !lse)) return MESA_ERR_INVALID_ARG;
+    if (a.Nk && (!dk.data || !dv.data)) return MESA_ERR_INVALID_ARG;
+    if (o.alpha || dO.alpha || (m.lo == nullptr) != (m.hi == nullptr) || !aligned16(o.data) || !aligned16(dO.data) || !aligned16(dq.data) || !aligned16(dk.data) ||
+        !aligned16(dv.data) || !aligned4(lse) || !aligned4(m.lo) || !aligned4(m.hi) || !aligned4(m.slopes) || !aligned4(m.q_start))
+        return MESA_ERR_INVALID_ARG;
+    if (!at_strides(a, a.Nq, group, o.batch, o.token, o.head) || !at_strides(a, a.Nq, group, dO.batch, dO.token, dO.head) ||
+        !at_strides(a, a.Nq, group, dq.batch, dq.token, dq.head) || !at_strides(a, a.Nk, 1, dk.batch, dk.token, dk.head) || !at_strides(a, a.Nk, 1, dv.batch, dv.token, dv.head))
+        return MESA_ERR_INVALID_ARG;
+    const AtBwdPlan p = at_bwd_plan(a, codes);
+    const int64_t heads = a.B * a.Hk, most = most_workgroups(256), quads = (a.Nq > a.Nk ? a.Nq * group : a.Nk * (group > 2 ? group : 2)) * (a.D / 4);
+    if (heads * p.key_blocks * p.splits > most || heads * (int64_t(p.blocks) + p.key_blocks) > most || heads * quads > most * kThreads) return MESA_ERR_UNSUPPORTED;
+    if (a.Nq > 0 && a.Nk > 0 && (!ws || !aligned16(ws) || ws_bytes < p.total)) return MESA_ERR_WORKSPACE;
+    AtBwd f;
+    f.s = at_shape(a, m);
+    auto view = [](const mesa_attention_in &x) { return AtView{static_cast<const char *>(x.data), x.batch * 2, x.token * 2, x.head * 2}; };
+    auto result = [](const mesa_attention_out &x) { return AtOut{static_cast<char *>(x.data), x.batch * 2, x.token * 2, x.head * 2}; };
+    f.q = view(q);
+    f.k = view(k);
+    f.v = view(v);
+    f.o = view(o);
+    f.dO = view(dO);
+    f.dq = result(dq);
+    f.dk = result(dk);
+    f.dv = result(dv);
+    f.lse = lse;
+    f.heads = uint32_t(heads);
+    f.key_blocks = p.key_blocks;
+    f.splits = p.splits;
+    f.row_blocks = p.row_blocks;
+    char *w = static_cast<char *>(ws);
+    const size_t h = size_t(heads), line = ab_up(h * p.rows * 4);
+    f.w.lse2 = reinterpret_cast<float *>(w);
+    f.w.delta = reinterpret_cast<float *>(w + line);
+    f.w.lo = reinterpret_cast<int32_t *>(w + 2 * line);
+    f.w.hi = reinterpret_cast<int32_t *>(w + 3 * line);
+    f.w.tiles = reinterpret_cast<int4 *>(w + 4 * line);
+    f.w.most = reinterpret_cast<float2 *>(w + 4 * line + ab_up(h * p.rows / 32 * sizeof(int4)));
+    f.w.values = reinterpret_cast<float *>(w + 4 * line + ab_up(h * p.rows / 32 * sizeof(int4)) + ab_up(h * p.blocks * sizeof(float2)));
+    f.w.rows = p.rows;
+    f.w.blocks = p.blocks;
+    f.w.key_blocks = p.key_blocks;
+    f.part = p.splits > 1 ? reinterpret_cast<float *>(w + p.info) : nullptr;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const bool bias = m.slopes != nullptr;
+    return dt == MESA_F16 ? at_bwd<_Float16>(a, f, p, in, codes, w, bias, s) : at_bwd<__bf16>(a, f, p, in, codes, w, bias, s);
+}

@@ -1,0 +1,446 @@
+// attention_fwd.hip -- the forward of attention over intervals of keys, and the intervals themselves.
+//   s = scale q.k (capped, biased by distance),  p = softmax over lo <= j < hi,  o = p v,  lse = log sum exp s
+//
+// One pass over the keys with a running maximum and sum (powers of two): a wave owns 32 rows -- queries of the heads that share
+// a key head, token by token, so that a group's heads read each tile once -- and keeps q and the sums of o in registers;
+// the workgroup's waves share tiles of k and v in LDS, the next tile on its way while one is worked on.  Scores come out
+// transposed (attention.hpp), so a row's maximum and sum are a lane's own business but for one swap of half-waves.
+// Tiles that no row of the workgroup sees are not loaded, tiles that all rows of a wave see in full are not masked.
+#include "attention.hpp"
+
+namespace mesa {
+
+AtShape at_shape(const mesa_attention &a, const mesa_attention_mask &m)
+{
+    AtShape s;
+    s.B = int32_t(a.B);
+    s.Nq = int32_t(a.Nq);
+    s.Nk = int32_t(a.Nk);
+    s.Hq = int32_t(a.Hq);
+    s.Hk = int32_t(a.Hk);
+    s.G = int32_t(a.Hq / a.Hk);
+    s.D = int32_t(a.D);
+    s.R = uint32_t(a.Nq * s.G);
+    s.div_g = make_fastdiv(uint32_t(s.G));
+    s.c = a.cap > 0.0f ? 2.0f * kLog2e * a.scale / a.cap : kLog2e * a.scale;
+    s.cap2 = a.cap * kLog2e;
+    s.scale = a.scale;
+    s.lo = m.lo;
+    s.hi = m.hi;
+    s.q_start = m.q_start;
+    s.slopes = m.slopes;
+    return s;
+}
+
+// ---------------------------------------------------------------------------------------------
+// intervals
+// ---------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(kThreads) void k_attn_bounds(int32_t *__restrict__ lo, int32_t *__restrict__ hi, int64_t Nq, int64_t Nk, int causal, int64_t window,
+                                                          const int32_t *__restrict__ kv_len, const int32_t *__restrict__ q_start, const int32_t *__restrict__ prefix,
+                                                          const int32_t *__restrict__ doc, uint32_t blocks_per_row)
+{
+    const int64_t b = blockIdx.x / blocks_per_row, i = int64_t(blockIdx.x - b * blocks_per_row) * kThreads + threadIdx.x;
+    if (i >= Nq) return;
+    int64_t n = Nk;
+    if (kv_len) n = kv_len[b] < n ? kv_len[b] : n;
+    const int64_t p = (q_start ? q_start[b] : Nk - Nq) + i;
+    int64_t l = 0, h = n;
+    if (p < 0 || p >= n) {
+        h = 0;
+    } else {
+        if (causal) {
+            int64_t seen = p + 1;
+            if (prefix && prefix[b] > seen) seen = prefix[b];
+            h = seen < h ? seen : h;
+        }
+        if (window > 0) {
+            l = p - window + 1 > 0 ? p - window + 1 : 0;
+            if (!causal && p + window < h) h = p + window;
+        }
+        if (doc) {
+            const int32_t *d = doc + b * Nk;
+            const int32_t mine = d[p];
+            // first key of the run: below p, numbers not smaller than mine; first key behind it: above p, larger ones
+            int64_t x = 0, y = p;
+            while (x < y) {
+                const int64_t c = (x + y) >> 1;
+                if (d[c] < mine) x = c + 1;
+                else y = c;
+            }
+            l = x > l ? x : l;
+            x = p + 1;
+            y = Nk;
+            while (x < y) {
+                const int64_t c = (x + y) >> 1;
+                if (d[c] > mine) y = c;
+                else x = c + 1;
+            }
+            h = x < h ? x : h;
+        }
+        if (l >= h) l = h = 0;
+    }
+    lo[b * Nq + i] = int32_t(l);
+    hi[b * Nq + i] = int32_t(h);
+}
+
+// ---------------------------------------------------------------------------------------------
+// forward
+// ---------------------------------------------------------------------------------------------
+struct AtFwd {
+    AtShape s;
+    AtView q, k, v;
+    AtOut o;
+    float *lse;
+    float *part_o, *part_lse;    // [split][(b, key head, row)][D] and [split][...]; null: no split
+    uint32_t heads, row_blocks, splits;   // heads: B * Hk
+};
+
+// NW waves of 32 rows, tiles of BN keys
+template <typename T, int DP, int NW, int BN, bool CAP, bool BIAS>
+__global__ __launch_bounds__(NW * 64, 2) void k_attn_fwd(const AtFwd a)
+{
+    typedef AtNum<T> Num;
+    typedef AtTile<NW * 64, BN, DP> Tile;
+    constexpr int kKs = DP / 16, kDt = DP / 32, kSub = BN / 32;
+    __shared__ __attribute__((aligned(16))) char lds[4 * Tile::kBytes];      // two tiles of k, two of v
+    __shared__ int range[2][NW];
+    const AtShape &s = a.s;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), half = lane >> 5;
+    const uint32_t head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads;     // the heads first: a head's workgroups stay on one XCD where they are a multiple of 8
+    const uint32_t split = rest % a.splits, rb = a.row_blocks - 1 - rest / a.splits;   // the longest rows of a causal order first
+    const int b = int(head / uint32_t(s.Hk)), hk = int(head) - b * s.Hk;
+    const uint32_t r_own = (rb * NW + wave) * 32 + (lane & 31), r = r_own < s.R ? r_own : s.R - 1;
+    const AtRow row = at_row(s, r);
+    const int hq = hk * s.G + int(row.g);
+    int lo, hi;
+    at_interval(s, b, row.token, lo, hi);
+    const bool none = lo >= hi;
+    const int wlo = at_wave_min(none ? 0x7FFFFFFF : lo), whi = at_wave_max(hi);   // of what the wave's rows see, any
+    const int flo = at_wave_max(lo), fhi = at_wave_min(hi);                        // and all
+    if (lane == 0) {
+        range[0][wave] = wlo;
+        range[1][wave] = whi;
+    }
+    u32x4 qf[kKs];
+    {
+        const char *p = a.q.p + int64_t(b) * a.q.batch + int64_t(row.token) * a.q.token + int64_t(hq) * a.q.head;
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) qf[ks] = at_column(p, ks, lane, s.D);
+    }
+    const float slope2 = BIAS ? s.slopes[hq] * kLog2e : 0.0f;
+    const int place = BIAS ? at_place(s, b, row.token) : 0;
+    __syncthreads();
+    int blo = 0x7FFFFFFF, bhi = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        blo = range[0][w] < blo ? range[0][w] : blo;
+        bhi = range[1][w] > bhi ? range[1][w] : bhi;
+    }
+    int t0 = bhi > 0 ? blo / BN : 0, t1 = bhi > 0 ? (bhi + BN - 1) / BN : 0;
+    if (a.splits > 1) {
+        const int per = (t1 - t0 + int(a.splits) - 1) / int(a.splits);
+        t0 += int(split) * per;
+        t1 = t0 + per < t1 ? t0 + per : t1;
+    }
+    t0 = __builtin_amdgcn_readfirstlane(t0);
+    t1 = __builtin_amdgcn_readfirstlane(t1);
+
+    const char *kbase = a.k.p + int64_t(b) * a.k.batch + int64_t(hk) * a.k.head, *vbase = a.v.p + int64_t(b) * a.v.batch + int64_t(hk) * a.v.head;
+    Tile tk, tv;
+    auto fetch = [&](int t) __attribute__((always_inline)) {
+        const int j0 = t * BN;
+        tk.load(kbase + int64_t(j0) * a.k.token, s.Nk - j0, s.D, [&](int x) { return x * int(a.k.token); });
+        tv.load(vbase + int64_t(j0) * a.v.token, s.Nk - j0, s.D, [&](int x) { return x * int(a.v.token); });
+    };
+
+    at_acc o[kDt];
+#pragma unroll
+    for (int d = 0; d < kDt; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    float m = kAtLow, l = 0.0f;
+
+    auto work = [&](const char *lk, const char *lv, int j0, auto masked) __attribute__((always_inline)) {
+        constexpr bool kMasked = decltype(masked)::value;
+        at_acc x[kSub];
+#pragma unroll
+        for (int t = 0; t < kSub; ++t) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[t][i] = 0.0f;
+#pragma unroll
+            for (int ks = 0; ks < kKs; ++ks) x[t] = Num::mfma(at_plain<DP>(lk, t * 32, ks, lane), qf[ks], x[t]);
+        }
+        const int first = j0 + 4 * half;           // the key of register 0
+        u32x4 seen[2 * kSub];
+        if (CAP || BIAS) {
+            const float away = float(place - first);
+#pragma unroll
+            for (int t = 0; t < kSub; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    if (CAP) x[t][i] = s.cap2 * at_tanh(x[t][i] * s.c);
+                    else x[t][i] *= s.c;
+                    if (BIAS) x[t][i] = fmaf(-slope2, fabsf(away - float(t * 32 + at_reg_row(i))), x[t][i]);
+                }
+        }
+        if (kMasked) {
+#pragma unroll
+            for (int t = 0; t < kSub; ++t)
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    bool vis[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int j = first + t * 32 + at_reg_row(8 * g + e);
+                        vis[e] = uint32_t(j - lo) < uint32_t(hi - lo);
+                        x[t][8 * g + e] = vis[e] ? x[t][8 * g + e] : -__builtin_inff();
+                    }
+                    seen[2 * t + g] = at_seen(vis, lane);
+                }
+        }
+        float top = x[0][0];
+#pragma unroll
+        for (int t = 0; t < kSub; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, x[t][i]);
+        top = at_pair_max(top);
+        constexpr bool kRaw = !CAP && !BIAS;       // the factor c is then still to come (c > 0)
+        if (kRaw) top *= s.c;
+        // the sums are scaled anew only where a row's maximum has grown by more than 2^8: probabilities up to 2^8 are as exact
+        if (__ballot(top > m + 8.0f)) {
+            const float m1 = fmaxf(m, top), f = at_exp2(m - m1);
+            m = m1;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < kDt; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= f;
+        }
+        u32x4 p[2 * kSub];
+        float l1 = 0.0f;
+#pragma unroll
+        for (int t = 0; t < kSub; ++t)
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int i = 8 * g + 2 * w;
+                    const float e0 = at_exp2(kRaw ? fmaf(x[t][i], s.c, -m) : x[t][i] - m), e1 = at_exp2(kRaw ? fmaf(x[t][i + 1], s.c, -m) : x[t][i + 1] - m);
+                    l += e0;
+                    l1 += e1;
+                    p[2 * t + g][w] = Num::pack(e0, e1);
+                }
+        l += l1;
+#pragma unroll
+        for (int g = 0; g < 2 * kSub; ++g)
+#pragma unroll
+            for (int d = 0; d < kDt; ++d) {
+                u32x4 f = at_transposed<DP>(lv, g * 16, d * 32, lane);
+                if (kMasked) f &= seen[g];
+                o[d] = Num::mfma(f, p[g], o[d]);
+            }
+    };
+
+    if (t0 < t1) fetch(t0);
+    for (int t = t0, cur = 0; t < t1; ++t, cur ^= 1) {
+        char *lk = lds + cur * 2 * Tile::kBytes, *lv = lk + Tile::kBytes;
+        tk.store(lk);
+        tv.store(lv);
+        __syncthreads();                            // the other pair of tiles is behind every wave then
+        if (t + 1 < t1) fetch(t + 1);
+        const int j0 = t * BN;
+        if (j0 + BN <= wlo || j0 >= whi) continue;
+        if (j0 >= flo && j0 + BN <= fhi) work(lk, lv, j0, std::false_type());
+        else work(lk, lv, j0, std::true_type());
+    }
+
+    l = at_pair_sum(l);
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    if (r_own >= s.R) return;
+    if (a.part_o) {
+        const int64_t at = int64_t(split) * a.heads * s.R + int64_t(head) * s.R + r;
+        if (half == 0) a.part_lse[at] = l > 0.0f ? m + __log2f(l) : -__builtin_inff();
+#pragma unroll
+        for (int d = 0; d < kDt; ++d)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int e = d * 32 + 8 * w + 4 * half;
+                if (e < s.D) *reinterpret_cast<float4 *>(a.part_o + at * s.D + e) = make_float4(o[d][4 * w] * inv, o[d][4 * w + 1] * inv, o[d][4 * w + 2] * inv, o[d][4 * w + 3] * inv);
+            }
+        return;
+    }
+    if (half == 0) a.lse[(int64_t(b) * s.Hq + hq) * s.Nq + row.token] = l > 0.0f ? (m + __log2f(l)) * kLn2 : -__builtin_inff();
+    char *op = a.o.p + int64_t(b) * a.o.batch + int64_t(row.token) * a.o.token + int64_t(hq) * a.o.head;
+#pragma unroll
+    for (int d = 0; d < kDt; ++d)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int e = d * 32 + 8 * w + 4 * half;
+            if (e < s.D) at_store4<T>(op + e * 2, o[d][4 * w] * inv, o[d][4 * w + 1] * inv, o[d][4 * w + 2] * inv, o[d][4 * w + 3] * inv);
+        }
+}
+
+// the splits of a row joined: weights 2^(lse_s - max), four elements per thread
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_attn_join(const AtFwd a, int64_t pieces)
+{
+    const AtShape &s = a.s;
+    const int64_t id = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+    if (id >= pieces) return;
+    const int quads = s.D / 4;
+    const int64_t at = id / quads;                       // (b, key head, row)
+    const int e = int(id - at * quads) * 4;
+    const int64_t step = int64_t(a.heads) * s.R;
+    float top = -__builtin_inff();
+    for (uint32_t k = 0; k < a.splits; ++k) top = fmaxf(top, a.part_lse[k * step + at]);
+    float total = 0.0f, x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (top > -__builtin_inff())
+        for (uint32_t k = 0; k < a.splits; ++k) {
+            const float w = at_exp2(a.part_lse[k * step + at] - top);
+            const float4 v = *reinterpret_cast<const float4 *>(a.part_o + (k * step + at) * s.D + e);
+            total += w;
+            x[0] = fmaf(w, v.x, x[0]);
+            x[1] = fmaf(w, v.y, x[1]);
+            x[2] = fmaf(w, v.z, x[2]);
+            x[3] = fmaf(w, v.w, x[3]);
+        }
+    const float inv = total > 0.0f ? 1.0f / total : 0.0f;
+    const uint32_t head = uint32_t(at / s.R), r = uint32_t(at - int64_t(head) * s.R);
+    const int b = int(head) / s.Hk, hk = int(head) - b * s.Hk;
+    const AtRow row = at_row(s, r);
+    const int hq = hk * s.G + int(row.g);
+    at_store4<T>(a.o.p + int64_t(b) * a.o.batch + int64_t(row.token) * a.o.token + int64_t(hq) * a.o.head + e * 2, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+    if (e == 0) a.lse[(int64_t(b) * s.Hq + hq) * s.Nq + row.token] = total > 0.0f ? (top + __log2f(total)) * kLn2 : -__builtin_inff();
+}
+
+struct AtFwdPlan {
+    int waves, keys;             // of a workgroup; of a tile
+    uint32_t row_blocks, splits;
+    size_t ws;
+};
+// Rows that fit one wave get workgroups of one wave with small tiles (a single token's reading is all latency and bandwidth, and
+// four waves would load for one); few workgroups share out the keys.
+static AtFwdPlan at_fwd_plan(const mesa_attention &a)
+{
+    AtFwdPlan p;
+    const int64_t R = a.Nq * (a.Hq / a.Hk), heads = a.B * a.Hk;
+    p.waves = R <= 32 ? 1 : 4;
+    p.keys = p.waves == 1 ? 32 : 64;
+    p.row_blocks = uint32_t(ceil_div(R, p.waves * 32));
+    const int64_t have = heads * p.row_blocks, want = p.waves == 1 ? 1536 : 384, most = a.Nk / (p.waves == 1 ? 256 : 512);
+    int64_t n = have > 0 ? want / have : 1;
+    n = n > most ? most : n;
+    n = n > 64 ? 64 : n < 1 ? 1 : n;
+    p.splits = uint32_t(n);
+    p.ws = n > 1 ? size_t(n) * size_t(heads) * size_t(R) * size_t(a.D + 1) * sizeof(float) : 0;
+    return p;
+}
+
+template <typename T, int DP, bool CAP, bool BIAS> static void at_fwd_launch(const AtFwd &a, const AtFwdPlan &p, hipStream_t s)
+{
+    const dim3 grid(a.heads * a.row_blocks * a.splits);
+    if (p.waves == 1) hipLaunchKernelGGL((k_attn_fwd<T, DP, 1, 32, CAP, BIAS>), grid, dim3(64), 0, s, a);
+    else hipLaunchKernelGGL((k_attn_fwd<T, DP, 4, 64, CAP, BIAS>), grid, dim3(256), 0, s, a);
+}
+template <typename T, int DP> static void at_fwd_forms(const AtFwd &a, const AtFwdPlan &p, bool cap, bool bias, hipStream_t s)
+{
+    if (cap && bias) at_fwd_launch<T, DP, true, true>(a, p, s);
+    else if (cap) at_fwd_launch<T, DP, true, false>(a, p, s);
+    else if (bias) at_fwd_launch<T, DP, false, true>(a, p, s);
+    else at_fwd_launch<T, DP, false, false>(a, p, s);
+}
+
+// zero output where there are no keys
+template <typename T> __global__ __launch_bounds__(kThreads) void k_attn_nothing(const AtFwd a, int64_t pieces)
+{
+    const AtShape &s = a.s;
+    const int64_t id = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+    if (id >= pieces) return;
+    const int quads = s.D / 4;
+    const int64_t at = id / quads, t = at / s.Hq, b = t / s.Nq;
+    const int h = int(at - t * s.Hq), e = int(id - at * quads) * 4, i = int(t - b * s.Nq);
+    at_store4<T>(a.o.p + b * a.o.batch + int64_t(i) * a.o.token + int64_t(h) * a.o.head + e * 2, 0.0f, 0.0f, 0.0f, 0.0f);
+    if (e == 0) a.lse[(b * s.Hq + h) * s.Nq + i] = -__builtin_inff();
+}
+
+}  // namespace mesa
+
+using namespace mesa;
+
+extern "C" MESA_EXPORT mesa_status mesa_attention_bounds(int32_t *lo, int32_t *hi, int64_t B, int64_t Nq, int64_t Nk, int causal, int64_t window, const int32_t *kv_len,
+                                                         const int32_t *q_start, const int32_t *prefix, const int32_t *doc, void *stream)
+{
+    const int64_t top = int64_t(1) << 30;
+    if (B < 0 || Nq < 0 || Nk < 0 || window < 0) return MESA_ERR_INVALID_ARG;
+    if (B == 0 || Nq == 0) return MESA_OK;
+    if (!lo || !hi || lo == hi || !aligned4(lo) || !aligned4(hi) || !aligned4(kv_len) || !aligned4(q_start) || !aligned4(prefix) || !aligned4(doc)) return MESA_ERR_INVALID_ARG;
+    if (Nq >= top || Nk >= top || B >= (int64_t(1) << 40) / Nq || B * ceil_div(Nq, kThreads) > most_workgroups(kThreads)) return MESA_ERR_UNSUPPORTED;
+    const uint32_t per = uint32_t(ceil_div(Nq, kThreads));
+    hipLaunchKernelGGL(k_attn_bounds, dim3(uint32_t(B) * per), dim3(kThreads), 0, static_cast<hipStream_t>(stream), lo, hi, Nq, Nk, causal, window < top ? window : top, kv_len,
+                       q_start, prefix, doc, per);
+    return launch_status();
+}
+
+extern "C" MESA_EXPORT size_t mesa_attention_fwd_workspace_bytes(mesa_attention a, mesa_dtype dt)
+{
+    return at_supported(a, dt) == MESA_OK && a.B > 0 && a.Nq > 0 ? at_fwd_plan(a).ws : 0;
+}
+
+namespace mesa {
+bool at_strides(const mesa_attention &a, int64_t tokens, int64_t heads, int64_t batch, int64_t token, int64_t head)
+{
+    const int64_t top = int64_t(1) << 30;
+    if (((batch | token | head) & 7) || batch < 0 || token < 0 || head < 0) return false;
+    return token <= top / 256 && head <= top / heads && 256 * token + heads * head + a.D < top && (tokens == 0 || batch < (int64_t(1) << 50));
+}
+}
+
+extern "C" MESA_EXPORT mesa_status mesa_attention_fwd(mesa_attention a, mesa_attention_in q, mesa_attention_in k, mesa_attention_in v, mesa_attention_out o, float *lse,
+                                                      mesa_attention_mask m, void *ws, size_t ws_bytes, mesa_dtype dt, void *stream)
+{
+    if (const mesa_status st = at_supported(a, dt)) return st;
+    if (a.B == 0 || a.Nq == 0) return MESA_OK;
+    if (!q.data || !o.data || !lse || (a.Nk && (!k.data || !v.data)) || q.alpha || k.alpha || v.alpha || (m.lo == nullptr) != (m.hi == nullptr)) return MESA_ERR_INVALID_ARG;
+    if (!aligned16(q.data) || !aligned16(k.data) || !aligned16(v.data) || !aligned16(o.data) || !aligned4(lse) || !aligned4(m.lo) || !aligned4(m.hi) || !aligned4(m.slopes) ||
+        !aligned4(m.q_start))
+        return MESA_ERR_INVALID_ARG;
+    const int64_t group = a.Hq / a.Hk;
+    if (!at_strides(a, a.Nq, group, q.batch, q.token, q.head) || !at_strides(a, a.Nk, 1, k.batch, k.token, k.head) || !at_strides(a, a.Nk, 1, v.batch, v.token, v.head) ||
+        !at_strides(a, a.Nq, group, o.batch, o.token, o.head))
+        return MESA_ERR_INVALID_ARG;
+    const AtFwdPlan p = at_fwd_plan(a);
+    const int64_t groups = a.B * a.Hk, quads = groups * a.Nq * group * (a.D / 4);
+    if (groups * p.row_blocks * p.splits > most_workgroups(256) || ceil_div(quads, kThreads) > most_workgroups(kThreads)) return MESA_ERR_UNSUPPORTED;
+    if (p.ws && (!ws || !aligned16(ws) || ws_bytes < p.ws)) return MESA_ERR_WORKSPACE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    AtFwd f;
+    f.s = at_shape(a, m);
+    auto view = [](const mesa_attention_in &x) { return AtView{static_cast<const char *>(x.data), x.batch * 2, x.token * 2, x.head * 2}; };
+    f.q = view(q);
+    f.k = view(k);
+    f.v = view(v);
+    f.o = AtOut{static_cast<char *>(o.data), o.batch * 2, o.token * 2, o.head * 2};
+    f.lse = lse;
+    f.heads = uint32_t(groups);
+    f.row_blocks = p.row_blocks;
+    f.splits = p.splits;
+    f.part_o = p.splits > 1 ? static_cast<float *>(ws) : nullptr;
+    f.part_lse = p.splits > 1 ? f.part_o + size_t(p.splits) * size_t(groups) * f.s.R * size_t(a.D) : nullptr;
+    const bool half = dt == MESA_F16;
+    const dim3 flat(uint32_t(ceil_div(quads, kThreads)));
+    if (a.Nk == 0) {
+        if (half) hipLaunchKernelGGL(k_attn_nothing<_Float16>, flat, dim3(kThreads), 0, s, f, quads);
+        else hipLaunchKernelGGL(k_attn_nothing<__bf16>, flat, dim3(kThreads), 0, s, f, quads);
+        return launch_status();
+    }
+    const bool cap = a.cap > 0.0f, bias = m.slopes != nullptr;
+    if (half) a.D <= 64 ? at_fwd_forms<_Float16, 64>(f, p, cap, bias, s) : at_fwd_forms<_Float16, 128>(f, p, cap, bias, s);
+    else a.D <= 64 ? at_fwd_forms<__bf16, 64>(f, p, cap, bias, s) : at_fwd_forms<__bf16, 128>(f, p, cap, bias, s);
+    if (const mesa_status st = launch_status()) return st;
+    if (p.splits > 1) {
+        if (half) hipLaunchKernelGGL(k_attn_join<_Float16>, flat, dim3(kThreads), 0, s, f, quads);
+        else hipLaunchKernelGGL(k_attn_join<__bf16>, flat, dim3(kThreads), 0, s, f, quads);
+        return launch_status();
+    }
+    return MESA_OK;
+}

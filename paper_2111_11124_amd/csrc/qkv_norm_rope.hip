@@ -1,0 +1,489 @@
+// qkv_norm_rope.hip -- the packed query/key/value projection of a language model's attention block: the norm of each query
+// and key head and the rotation by position in one pass that also leaves the codes of every head and moves the running
+// estimates; queries and keys again from the codes; and the backward from the codes.
+//   r = 1/sqrt(sum x^2/D + eps),  z = gamma x r,  y = R(pos) z;     g = R(pos)^T dy,  n = x_hat r,  u = gamma g,
+//   dx = r (u - n mean(u n)),  dgamma = sum g n
+// R turns pairs of elements, so its transpose is the same rotation by the negative angle.
+//
+// Bound by memory: per element of a 16-bit tensor the forward moves 2 bytes in and 2 + 1 out, the backward 2 + 1 in and 2 out.
+// A head is a group of LPH lanes with eight elements each (LPH: the power of two from D/8), a wave holds 64/LPH heads side by
+// side ("slot") and walks over the tokens of its tile with the same heads, so that alpha, beta, gamma stay in
+// registers and the extrema accumulate there.  Cosines and sines depend on token and pair, not on the head: a workgroup
+// forms them once per tile into LDS -- angle and reduction in binary64, as positions times frequencies have more than 24
+// bits -- and all heads read them there.
+#include <hip/hip_runtime.h>
+
+#include "api_util.hpp"
+#include "common.hpp"
+#include "quantize.hpp"
+
+namespace mesa {
+
+constexpr int kQkvTile = 32;        // tokens of a tile at most (cosines and sines of 32 x 128 pairs: 32 KB)
+constexpr int kQkvGrid = 1024;      // workgroups at most: four per compute unit
+constexpr int kQkvMaxHeads = 512;
+constexpr int kQkvU = 4;            // tokens in flight per wave
+
+struct QkvGeom {
+    int64_t T;
+    uint32_t Hq, Hn, H, D, rot, lph_log2;   // Hn = Hq + Hk, H = Hn + Hv
+    uint32_t tile, phases_log2;             // tokens per tile; into how many parts the four waves share out a tile's tokens
+    uint32_t end[4];                        // first pair behind each axis
+    int interleaved;
+    float eps;
+};
+
+static QkvGeom qkv_geom(const mesa_qkv_heads &h)
+{
+    QkvGeom g;
+    g.T = h.T;
+    g.Hq = uint32_t(h.Hq);
+    g.Hn = uint32_t(h.Hq + h.Hk);
+    g.H = uint32_t(h.Hq + h.Hk + h.Hv);
+    g.D = uint32_t(h.D);
+    g.rot = uint32_t(h.rot);
+    g.lph_log2 = 0;
+    while ((8u << g.lph_log2) < g.D) ++g.lph_log2;
+    // few tokens: tiles of fewer, so that there are workgroups for every compute unit
+    int64_t t = ceil_div(h.T, kQkvGrid);
+    g.tile = uint32_t(t < 1 ? 1 : t > kQkvTile ? kQkvTile : t);
+    const uint32_t slots = (g.H << g.lph_log2) / 64 + (((g.H << g.lph_log2) % 64) != 0);
+    g.phases_log2 = slots >= 4 ? 0 : slots >= 2 ? 1 : 2;
+    uint32_t e = 0;
+    for (int a = 0; a < 4; ++a) {
+        if (a < h.axes) e += uint32_t(h.section[a]);
+        g.end[a] = a < h.axes - 1 ? e : 0xFFFFFFFFu;
+    }
+    g.interleaved = h.interleaved;
+    g.eps = h.eps;
+    return g;
+}
+
+static int qkv_grid(const QkvGeom &g)
+{
+    const int64_t n = ceil_div(g.T, g.tile);
+    return int(n < kQkvGrid ? n : kQkvGrid);
+}
+
+// cosines and sines of a tile's tokens, [token][pair]
+__device__ __forceinline__ void qkv_angles(float2 *cs, const QkvGeom &g, const float *__restrict__ freq, const int32_t *__restrict__ pos, int64_t t0, uint32_t tokens)
+{
+    const uint32_t half = g.rot / 2;
+    for (uint32_t k = threadIdx.x; k < tokens * half; k += kThreads) {
+        const uint32_t tk = k / half, i = k - tk * half;
+        const uint32_t axis = (i >= g.end[0]) + (i >= g.end[1]) + (i >= g.end[2]);
+        // in turns, the whole ones taken off: what is left is below a half and exact enough in binary32 (2^-25 turns)
+        double turns = double(pos[int64_t(axis) * g.T + t0 + tk]) * double(freq[i]) * 0.15915494309189535;
+        turns -= rint(turns);
+        float s, c;
+        sincospif(float(2.0 * turns), &s, &c);
+        cs[k] = make_float2(c, s);
+    }
+}
+
+// f[0..7] of this lane's part of a head, turned by the token's angles; d0: the part's first element.  sign -1: turned back.
+// Every lane of the wave takes part (the partner's elements come from its registers).
+__device__ __forceinline__ void qkv_turn(float f[8], const float2 *cs, uint32_t d0, uint32_t rot, int interleaved, int partner, float sign)
+{
+    if (interleaved) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t i = d0 / 2 + k;
+            if (2 * i < rot) {
+                const float2 w = cs[i];
+                const float a = f[2 * k], b = f[2 * k + 1], s = sign * w.y;
+                f[2 * k] = fmaf(a, w.x, -(b * s));
+                f[2 * k + 1] = fmaf(b, w.x, a * s);
+            }
+        }
+        return;
+    }
+    const bool second = d0 >= rot / 2, turned = d0 < rot;
+    const float2 *p = cs + (turned ? (second ? d0 - rot / 2 : d0) : 0);
+    const float sg = second ? sign : -sign;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float other = __shfl(f[k], partner, 64);
+        const float2 w = p[k];
+        const float v = fmaf(f[k], w.x, other * (sg * w.y));
+        f[k] = turned ? v : f[k];
+    }
+}
+
+__device__ __forceinline__ float qkv_head_sum(float v, uint32_t lph_log2)
+{
+    for (uint32_t k = 0; k < lph_log2; ++k) v += __shfl_xor(v, 1 << k, 64);
+    return v;
+}
+
+__device__ __forceinline__ void qkv_hat(u32x2 c, float s, float b, float f[8])
+{
+    codes_to_float(c, f);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) f[k] = fmaf(f[k], s, b);
+}
+
+// The forward (AGAIN false: from x, with codes and extrema) or queries and keys once more (AGAIN: from the codes and rstd).
+// Both round y once, from binary32.
+template <typename T, bool SR, bool AGAIN>
+__global__ __launch_bounds__(kThreads) void k_qkv_fwd(QkvGeom g, const void *__restrict__ x, int64_t x_row, const int8_t *__restrict__ qin, const void *__restrict__ gamma_q,
+                                                      const void *__restrict__ gamma_k, const float *__restrict__ freq, const int32_t *__restrict__ pos,
+                                                      const float *__restrict__ alpha, const float *__restrict__ beta, void *__restrict__ y, float *__restrict__ rstd,
+                                                      int8_t *__restrict__ q, uint64_t seed, uint64_t offset, float *__restrict__ part)
+{
+    typedef typename Store<T>::raw_t Raw;
+    extern __shared__ float2 smem[];
+    float2 *cs = smem;
+    int *lmn = reinterpret_cast<int *>(smem + g.tile * (g.rot / 2)), *lmx = lmn + g.H;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint32_t lph = 1u << g.lph_log2, hpw = 64u >> g.lph_log2;
+    const uint32_t d0 = (lane & (lph - 1)) * 8, sub = lane >> g.lph_log2;
+    const int hop = int(g.rot / 16), partner = int(lane) + (d0 < g.rot / 2 ? hop : d0 < g.rot ? -hop : 0);
+    const uint32_t heads = AGAIN ? g.Hn : g.H, slots = (heads + hpw - 1) / hpw;
+    const uint32_t phase = wave & ((1u << g.phases_log2) - 1), phases = 1u << g.phases_log2;
+    const float inv_d = 1.0f / float(g.D);
+    if (!AGAIN)
+        for (uint32_t h = threadIdx.x; h < g.H; h += kThreads) {
+            lmn[h] = order_key(__builtin_inff());
+            lmx[h] = order_key(-__builtin_inff());
+        }
+    for (int64_t t0 = int64_t(blockIdx.x) * g.tile; t0 < g.T; t0 += int64_t(gridDim.x) * g.tile) {
+        const uint32_t tokens = g.T - t0 < g.tile ? uint32_t(g.T - t0) : g.tile;
+        __syncthreads();                           // the last tile's angles are done with
+        qkv_angles(cs, g, freq, pos, t0, tokens);
+        __syncthreads();
+        for (uint32_t slot = wave >> g.phases_log2; slot < slots; slot += (kThreads / 64) >> g.phases_log2) {
+            const uint32_t hd = slot * hpw + sub;
+            const bool act = hd < heads && d0 < g.D, turn = hd < g.Hn;
+            const bool any_turn = slot * hpw < g.Hn;     // uniform
+            float r = 0.0f, b = 0.0f, gam[8];
+            if (act) {
+                b = beta[hd];
+                r = alpha[hd];
+                r = AGAIN ? r / 255.0f : r > 0.0f ? 255.0f / r : 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) gam[k] = 1.0f;
+            if (gamma_q && act && turn) Store<T>::unpack(Store<T>::load(hd < g.Hq ? gamma_q : gamma_k, d0), gam);
+            float mn = __builtin_inff(), mx = -__builtin_inff();
+            for (uint32_t base = phase; base < tokens; base += phases * kQkvU) {
+                Raw raw[kQkvU];
+                u32x2 cin[kQkvU];
+                float rs[kQkvU];
+#pragma unroll
+                for (int u = 0; u < kQkvU; ++u) {
+                    const uint32_t tk = base + u * phases;
+                    const int64_t t = t0 + (tk < tokens ? tk : base);       // past the tile: its first token again, not stored
+                    if (AGAIN) {
+                        cin[u] = act ? nt_load<u32x2>(qin + (t * g.H + hd) * g.D + d0) : u32x2{0u, 0u};
+                        rs[u] = gamma_q && act ? rstd[t * g.Hn + hd] : 1.0f;
+                    } else {
+                        raw[u] = act ? Nt<T>::load(x, t * x_row + int64_t(hd) * g.D + d0) : Raw{};
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < kQkvU; ++u) {
+                    const uint32_t tk = base + u * phases;
+                    const bool live = act && tk < tokens;
+                    const int64_t t = t0 + (tk < tokens ? tk : base);
+                    float f[8];
+                    if (AGAIN) {
+                        qkv_hat(cin[u], r, b, f);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) f[k] *= rs[u] * gam[k];
+                    } else {
+                        Store<T>::unpack(raw[u], f);
+                        const int64_t e = (t * g.H + hd) * g.D + d0;
+                        float v[8], bits[8];
+                        if (SR) sr_bits(seed, offset + uint64_t(e >> 3), bits);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            v[k] = quantize_real<SR>(f[k], r, b, SR ? bits[k] : 0.0f);
+                            mn = vmin(mn, f[k]);
+                            mx = vmax(mx, f[k]);
+                        }
+                        const u32x2 c = round_pack_codes<SR>(v);
+                        if (live) nt_store<u32x2>(q + e, c);
+                        if (!any_turn) continue;
+                        if (gamma_q) {
+                            float ss = 0.0f;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) ss = fmaf(f[k], f[k], ss);
+                            const float rr = 1.0f / sqrtf(fmaf(qkv_head_sum(ss, g.lph_log2), inv_d, g.eps));
+                            if (live && turn && d0 == 0) rstd[t * g.Hn + hd] = rr;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) f[k] *= rr * gam[k];
+                        }
+                    }
+                    if (g.rot) qkv_turn(f, cs + (tk < tokens ? tk : base) * (g.rot / 2), d0, g.rot, g.interleaved, partner, 1.0f);
+                    if (live && turn) Nt<T>::store(y, (t * g.Hn + hd) * g.D + d0, Store<T>::pack(f));
+                }
+            }
+            if (!AGAIN && act) {
+                atomicMin(&lmn[hd], order_key(mn));
+                atomicMax(&lmx[hd], order_key(mx));
+            }
+        }
+    }
+    if (!AGAIN) {
+        __syncthreads();
+        for (uint32_t h = threadIdx.x; h < g.H; h += kThreads) {
+            part[int64_t(blockIdx.x) * 2 * g.H + h] = order_val(lmn[h]);
+            part[int64_t(blockIdx.x) * 2 * g.H + g.H + h] = order_val(lmx[h]);
+        }
+    }
+}
+
+// The backward; part[workgroup][2][D] takes the gains' gradients of its tokens, of query heads and of key heads.
+template <typename T, bool NORM>
+__global__ __launch_bounds__(kThreads) void k_qkv_bwd(QkvGeom g, const int8_t *__restrict__ q, const void *__restrict__ gamma_q, const void *__restrict__ gamma_k,
+                                                      const float *__restrict__ freq, const int32_t *__restrict__ pos, const float *__restrict__ alpha,
+                                                      const float *__restrict__ beta, const float *__restrict__ rstd, const void *dy, void *dx, int64_t dx_row,
+                                                      float *__restrict__ part)
+{
+    typedef typename Store<T>::raw_t Raw;
+    extern __shared__ float2 smem[];
+    float2 *cs = smem;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint32_t lph = 1u << g.lph_log2, hpw = 64u >> g.lph_log2;
+    const uint32_t d0 = (lane & (lph - 1)) * 8, sub = lane >> g.lph_log2;
+    const int hop = int(g.rot / 16), partner = int(lane) + (d0 < g.rot / 2 ? hop : d0 < g.rot ? -hop : 0);
+    const uint32_t slots = (g.Hn + hpw - 1) / hpw;
+    const uint32_t phase = wave & ((1u << g.phases_log2) - 1), phases = 1u << g.phases_log2;
+    const float inv_d = 1.0f / float(g.D);
+    float acc[2][8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) acc[0][k] = acc[1][k] = 0.0f;
+    for (int64_t t0 = int64_t(blockIdx.x) * g.tile; t0 < g.T; t0 += int64_t(gridDim.x) * g.tile) {
+        const uint32_t tokens = g.T - t0 < g.tile ? uint32_t(g.T - t0) : g.tile;
+        __syncthreads();
+        qkv_angles(cs, g, freq, pos, t0, tokens);
+        __syncthreads();
+        for (uint32_t slot = wave >> g.phases_log2; slot < slots; slot += (kThreads / 64) >> g.phases_log2) {
+            const uint32_t hd = slot * hpw + sub;
+            const bool act = hd < g.Hn && d0 < g.D, key = hd >= g.Hq;
+            float s = 0.0f, b = 0.0f, gam[8];
+            if (NORM && act) {
+                s = alpha[hd] / 255.0f;
+                b = beta[hd];
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) gam[k] = 0.0f;
+            if (NORM && act) Store<T>::unpack(Store<T>::load(key ? gamma_k : gamma_q, d0), gam);
+            float mine[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) mine[k] = 0.0f;
+            for (uint32_t base = phase; base < tokens; base += phases * kQkvU) {
+                Raw raw[kQkvU];
+                u32x2 cin[kQkvU];
+                float rs[kQkvU];
+#pragma unroll
+                for (int u = 0; u < kQkvU; ++u) {
+                    const uint32_t tk = base + u * phases;
+                    const int64_t t = t0 + (tk < tokens ? tk : base);
+                    raw[u] = act ? Nt<T>::load(dy, (t * g.Hn + hd) * g.D + d0) : Raw{};
+                    if (NORM) {
+                        cin[u] = act ? nt_load<u32x2>(q + (t * g.H + hd) * g.D + d0) : u32x2{0u, 0u};
+                        rs[u] = act ? rstd[t * g.Hn + hd] : 0.0f;
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < kQkvU; ++u) {
+                    const uint32_t tk = base + u * phases;
+                    const bool live = act && tk < tokens;
+                    const int64_t t = t0 + (tk < tokens ? tk : base);
+                    float f[8];
+                    Store<T>::unpack(raw[u], f);
+                    if (g.rot) qkv_turn(f, cs + (tk < tokens ? tk : base) * (g.rot / 2), d0, g.rot, g.interleaved, partner, -1.0f);
+                    if (NORM) {
+                        float n[8], dot = 0.0f;
+                        qkv_hat(cin[u], s, b, n);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            n[k] *= rs[u];
+                            if (live) mine[k] = fmaf(f[k], n[k], mine[k]);
+                            f[k] *= gam[k];
+                            dot = fmaf(f[k], n[k], dot);
+                        }
+                        const float mean = qkv_head_sum(act ? dot : 0.0f, g.lph_log2) * inv_d;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) f[k] = rs[u] * fmaf(-n[k], mean, f[k]);
+                    }
+                    if (live) Nt<T>::store(dx, t * dx_row + int64_t(hd) * g.D + d0, Store<T>::pack(f));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                acc[0][k] += key ? 0.0f : mine[k];
+                acc[1][k] += key ? mine[k] : 0.0f;
+            }
+        }
+    }
+    if (!NORM) return;
+    // lanes that hold the same elements of different heads, then the four waves, each in a fixed order
+    float *sum = reinterpret_cast<float *>(smem);        // [wave][2][8 * lph]
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            float v = acc[c][k];
+            for (uint32_t m = lph; m < 64; m <<= 1) v += __shfl_xor(v, int(m), 64);
+            if (sub == 0) sum[((wave * 2 + c) << (g.lph_log2 + 3)) + d0 + k] = v;
+        }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < 2 * g.D; i += kThreads) {
+        const uint32_t c = i >= g.D, d = i - c * g.D;
+        float v = 0.0f;
+        for (uint32_t w = 0; w < kThreads / 64; ++w) v += sum[((w * 2 + c) << (g.lph_log2 + 3)) + d];
+        part[int64_t(blockIdx.x) * 2 * g.D + i] = v;
+    }
+}
+
+// columns of part[nwg][2*D]: a workgroup takes 32 of them, 32 rows at a time
+constexpr int kQkvCols = 32;
+__global__ __launch_bounds__(1024) void k_qkv_gains(const float *__restrict__ part, int nwg, uint32_t D, float *__restrict__ dgamma_q, float *__restrict__ dgamma_k)
+{
+    __shared__ float s[32][kQkvCols + 1];
+    const uint32_t col = blockIdx.x * kQkvCols + (threadIdx.x & 31u), row = threadIdx.x >> 5;
+    float v = 0.0f;
+    if (col < 2 * D)
+#pragma unroll 8
+        for (int w = int(row); w < nwg; w += 32) v += part[int64_t(w) * 2 * D + col];
+    s[row][threadIdx.x & 31u] = v;
+    __syncthreads();
+    if (row == 0 && col < 2 * D) {
+        float a = 0.0f;
+        for (int k = 0; k < 32; ++k) a += s[k][threadIdx.x & 31u];
+        if (col < D) dgamma_q[col] = a;
+        else dgamma_k[col - D] = a;
+    }
+}
+
+static mesa_status check_qkv(const mesa_qkv_heads &h, mesa_dtype dt)
+{
+    if (!valid_dtype(dt) || h.T < 0 || h.Hq < 0 || h.Hk < 0 || h.Hv < 0 || h.Hq + h.Hk < 1 || h.D < 1 || h.rot < 0 || h.rot > h.D || (h.rot & 1)) return MESA_ERR_INVALID_ARG;
+    if (h.axes < 1 || h.axes > 4 || !(h.eps >= 0.0f) || !(h.eps <= 3.0e38f)) return MESA_ERR_INVALID_ARG;
+    int64_t pairs = 0;
+    for (int a = 0; a < h.axes; ++a) {
+        if (h.section[a] < 0 || h.section[a] > h.rot / 2) return MESA_ERR_INVALID_ARG;
+        pairs += h.section[a];
+    }
+    if (pairs != h.rot / 2) return MESA_ERR_INVALID_ARG;
+    if (h.Hq > kQkvMaxHeads || h.Hk > kQkvMaxHeads || h.Hv > kQkvMaxHeads || h.Hq + h.Hk + h.Hv > kQkvMaxHeads) return MESA_ERR_UNSUPPORTED;
+    if (h.D % 8 != 0 || h.D > 256 || (!h.interleaved && h.rot % 16 != 0) || h.T >= (int64_t(1) << 31)) return MESA_ERR_UNSUPPORTED;
+    return MESA_OK;
+}
+
+static size_t qkv_lds(const QkvGeom &g, bool extrema)
+{
+    size_t n = size_t(g.tile) * (g.rot / 2) * 8 + (extrema ? size_t(g.H) * 8 : 0);
+    const size_t sums = size_t(8) * (8u << g.lph_log2) * 4;      // the backward's four waves
+    return n > sums ? n : sums;
+}
+
+}  // namespace mesa
+
+using namespace mesa;
+
+extern "C" MESA_EXPORT size_t mesa_qkv_norm_rope_fwd_q_workspace_bytes(mesa_qkv_heads h, mesa_dtype dt)
+{
+    if (check_qkv(h, dt) != MESA_OK) return 0;
+    const QkvGeom g = qkv_geom(h);
+    return size_t(qkv_grid(g) < 1 ? 1 : qkv_grid(g)) * 2 * g.H * sizeof(float);
+}
+
+extern "C" MESA_EXPORT size_t mesa_qkv_norm_rope_bwd_q_workspace_bytes(mesa_qkv_heads h, mesa_dtype dt)
+{
+    if (check_qkv(h, dt) != MESA_OK) return 0;
+    const QkvGeom g = qkv_geom(h);
+    return size_t(qkv_grid(g) < 1 ? 1 : qkv_grid(g)) * 2 * g.D * sizeof(float);
+}
+
+extern "C" MESA_EXPORT mesa_status mesa_qkv_norm_rope_fwd_q(const void *x, int64_t x_row, mesa_qkv_heads h, const void *gamma_q, const void *gamma_k, const float *freq,
+                                                            const int32_t *pos, float *alpha, float *beta, float lambda, void *y, float *rstd, int8_t *q, mesa_round mode,
+                                                            uint64_t seed, uint64_t offset, void *ws, size_t ws_bytes, mesa_dtype dt, void *stream)
+{
+    if (mode != MESA_ROUND_NEAREST_EVEN && mode != MESA_ROUND_STOCHASTIC) return MESA_ERR_INVALID_ARG;
+    if (!(lambda >= 0.0f && lambda <= 1.0f)) return MESA_ERR_INVALID_ARG;
+    if (const mesa_status st = check_qkv(h, dt)) return st;
+    if (x_row % 8 != 0 || x_row < (h.Hq + h.Hk + h.Hv) * h.D || (gamma_q == nullptr) != (gamma_k == nullptr)) return MESA_ERR_INVALID_ARG;
+    if (h.T == 0) return MESA_OK;
+    if (x_row >= (int64_t(1) << 31)) return MESA_ERR_UNSUPPORTED;
+    if (!x || !y || !q || !alpha || !beta || x == y || !aligned16(x) || !aligned16(y) || !aligned16(q) || !aligned16(gamma_q) || !aligned16(gamma_k) || !aligned4(alpha) ||
+        !aligned4(beta) || (gamma_q && !rstd) || !aligned4(rstd) || (h.rot && (!freq || !pos)) || !aligned4(freq) || !aligned4(pos))
+        return MESA_ERR_INVALID_ARG;
+    const QkvGeom g = qkv_geom(h);
+    const int grid = qkv_grid(g);
+    if (!ws || !aligned4(ws) || ws_bytes < mesa_qkv_norm_rope_fwd_q_workspace_bytes(h, dt)) return MESA_ERR_WORKSPACE;
+    const size_t lds = qkv_lds(g, true);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+#define MESA_QKV(T) \
+    do { \
+        auto *k = mode == MESA_ROUND_STOCHASTIC ? k_qkv_fwd<T, true, false> : k_qkv_fwd<T, false, false>; \
+        hipLaunchKernelGGL(k, dim3(grid), dim3(kThreads), lds, s, g, x, x_row, nullptr, gamma_q, gamma_k, freq, pos, alpha, beta, y, rstd, q, seed, offset, static_cast<float *>(ws)); \
+    } while (0)
+    MESA_FOR_DTYPE(dt, MESA_QKV);
+#undef MESA_QKV
+    if (const mesa_status st = launch_status()) return st;
+    launch_ema_finalize(static_cast<const float *>(ws), grid, g.H, alpha, beta, lambda, 0, 0, 0.0f, s);
+    return launch_status();
+}
+
+extern "C" MESA_EXPORT mesa_status mesa_qkv_norm_rope_recompute_q(const int8_t *q, mesa_qkv_heads h, const void *gamma_q, const void *gamma_k, const float *freq,
+                                                                  const int32_t *pos, const float *alpha, const float *beta, const float *rstd, void *y, mesa_dtype dt,
+                                                                  void *stream)
+{
+    if (const mesa_status st = check_qkv(h, dt)) return st;
+    if ((gamma_q == nullptr) != (gamma_k == nullptr)) return MESA_ERR_INVALID_ARG;
+    if (h.T == 0) return MESA_OK;
+    if (!q || !y || !alpha || !beta || !aligned16(q) || !aligned16(y) || !aligned16(gamma_q) || !aligned16(gamma_k) || !aligned4(alpha) || !aligned4(beta) ||
+        (gamma_q && !rstd) || !aligned4(rstd) || (h.rot && (!freq || !pos)) || !aligned4(freq) || !aligned4(pos))
+        return MESA_ERR_INVALID_ARG;
+    const QkvGeom g = qkv_geom(h);
+    const size_t lds = qkv_lds(g, false);
+#define MESA_QKV(T) \
+    hipLaunchKernelGGL((k_qkv_fwd<T, false, true>), dim3(qkv_grid(g)), dim3(kThreads), lds, static_cast<hipStream_t>(stream), g, nullptr, 0, q, gamma_q, gamma_k, freq, pos, alpha, \
+                       beta, y, const_cast<float *>(rstd), nullptr, 0, 0, nullptr)
+    MESA_FOR_DTYPE(dt, MESA_QKV);
+#undef MESA_QKV
+    return launch_status();
+}
+
+extern "C" MESA_EXPORT mesa_status mesa_qkv_norm_rope_bwd_q(const int8_t *q, mesa_qkv_heads h, const void *gamma_q, const void *gamma_k, const float *freq, const int32_t *pos,
+                                                            const float *alpha, const float *beta, const float *rstd, const void *dy, void *dx, int64_t dx_row,
+                                                            float *dgamma_q, float *dgamma_k, void *ws, size_t ws_bytes, mesa_dtype dt, void *stream)
+{
+    if (const mesa_status st = check_qkv(h, dt)) return st;
+    const bool norm = gamma_q != nullptr;
+    if (norm != (gamma_k != nullptr) || dx_row % 8 != 0 || dx_row < (h.Hq + h.Hk) * h.D || (norm && (!dgamma_q || !dgamma_k)) || !aligned4(dgamma_q) || !aligned4(dgamma_k))
+        return MESA_ERR_INVALID_ARG;
+    if (dx == dy && dx_row != (h.Hq + h.Hk) * h.D) return MESA_ERR_INVALID_ARG;
+    if (dx_row >= (int64_t(1) << 31)) return MESA_ERR_UNSUPPORTED;
+    if (h.T > 0) {
+        if (!dy || !dx || !aligned16(dy) || !aligned16(dx) || (h.rot && (!freq || !pos)) || !aligned4(freq) || !aligned4(pos)) return MESA_ERR_INVALID_ARG;
+        if (norm && (!q || !alpha || !beta || !rstd || !aligned16(q) || !aligned16(gamma_q) || !aligned16(gamma_k) || !aligned4(alpha) || !aligned4(beta) || !aligned4(rstd)))
+            return MESA_ERR_INVALID_ARG;
+    }
+    if (h.T == 0 && !norm) return MESA_OK;
+    const QkvGeom g = qkv_geom(h);
+    const int grid = qkv_grid(g);
+    if (norm && (!ws || !aligned4(ws) || ws_bytes < mesa_qkv_norm_rope_bwd_q_workspace_bytes(h, dt))) return MESA_ERR_WORKSPACE;
+    const size_t lds = qkv_lds(g, false);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (h.T > 0) {
+#define MESA_QKV(T) \
+    do { \
+        auto *k = norm ? k_qkv_bwd<T, true> : k_qkv_bwd<T, false>; \
+        hipLaunchKernelGGL(k, dim3(grid), dim3(kThreads), lds, s, g, q, gamma_q, gamma_k, freq, pos, alpha, beta, rstd, dy, dx, dx_row, static_cast<float *>(ws)); \
+    } while (0)
+        MESA_FOR_DTYPE(dt, MESA_QKV);
+#undef MESA_QKV
+        if (const mesa_status st = launch_status()) return st;
+    }
+    if (norm) {   // no tokens: zeros
+        hipLaunchKernelGGL(k_qkv_gains, dim3(uint32_t(ceil_div(2 * h.D, kQkvCols))), dim3(1024), 0, s, static_cast<const float *>(ws), h.T > 0 ? grid : 0, g.D, dgamma_q, dgamma_k);
+        return launch_status();
+    }
+    return MESA_OK;
+}
