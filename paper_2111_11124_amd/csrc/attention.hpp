@@ -137,21 +137,29 @@ template <int NT, int ROWS, int DP> struct AtTile {
     }
 };
 
-// A operand, rows as they lie: rows row0..row0+31 of the tile, elements 16*ks ..+15
-template <int DP> __device__ __forceinline__ u32x4 at_plain(const char *lds, int row0, int ks, int lane)
+// LDS by its 32-bit address: a lane's place in a tile is one register for plain reads and one for transposing ones; which
+// piece a read takes is an exclusive-or with a constant (tiles start at multiples of 128 bytes), the row an immediate offset.
+__device__ __forceinline__ uint32_t at_address(const char *lds) { return uint32_t(uintptr_t((__attribute__((address_space(3))) const char *)lds)); }
+template <int DP> __device__ __forceinline__ uint32_t at_plain_lane(int lane) { return (lane & 31) * (DP * 2) + (((lane >> 5) ^ at_turn(lane & 31)) << 4); }
+template <int DP> __device__ __forceinline__ uint32_t at_trans_lane(int lane)
 {
-    const int row = row0 + (lane & 31), piece = ks * 2 + (lane >> 5);
-    return *reinterpret_cast<const u32x4 *>(lds + row * (DP * 2) + ((piece ^ at_turn(lane & 31)) << 4));
+    const int sl = lane & 15, row = 4 * (lane >> 5) + (sl >> 2), piece = ((lane >> 4) & 1) * 2 + ((sl & 3) >> 1);
+    return row * (DP * 2) + ((piece ^ at_turn(row)) << 4) + (sl & 1) * 8;
 }
-// A operand, transposed: elements d0..d0+31 as its rows, the tile's rows row0..row0+15 as the contracted index
-template <int DP> __device__ __forceinline__ u32x4 at_transposed(const char *lds, int row0, int d0, int lane)
+// A operand, rows as they lie: rows row0..row0+31 of the tile (row0 a multiple of 32), elements 16*ks ..+15; at: tile's address + at_plain_lane
+template <int DP> __device__ __forceinline__ u32x4 at_plain(uint32_t at, int row0, int ks)
 {
-    const int sl = lane & 15, h = lane >> 5;
-    const int row = row0 + 4 * h + (sl >> 2), col = d0 + ((lane >> 4) & 1) * 16 + (sl & 3) * 4;
-    const char *p = lds + row * (DP * 2) + (((col >> 3) ^ at_turn(4 * h + (sl >> 2))) << 4) + (col & 7) * 2;
-    typedef __attribute__((address_space(3))) at_v4s *lds_v4s;
-    const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)p));
-    const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(p + 8 * DP * 2)));
+    typedef __attribute__((address_space(3))) const u32x4 *lds_p;
+    return *(lds_p)((at ^ uint32_t((ks & 3) << 5)) + uint32_t(row0 * (DP * 2) + (ks >> 2) * 128));
+}
+// A operand, transposed: elements d0..d0+31 (d0 a multiple of 32) as its rows, the tile's rows row0..row0+15 (a multiple of 16) as the
+// contracted index; at: tile's address + at_trans_lane
+template <int DP> __device__ __forceinline__ u32x4 at_transposed(uint32_t at, int row0, int d0)
+{
+    typedef __attribute__((address_space(3))) at_v4s *lds_p;
+    const uint32_t p = (at ^ uint32_t((d0 & 32) << 1)) + uint32_t(row0 * (DP * 2) + (d0 >> 6) * 128);
+    const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)p));
+    const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)(p + 8 * DP * 2)));
     return u32x4{a[0], a[1], b[0], b[1]};
 }
 

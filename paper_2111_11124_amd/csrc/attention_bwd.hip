@@ -193,7 +193,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
     typedef AtNum<T> Num;
     typedef AtTile<NW * 64, BN, DP> Tile;
     constexpr int kKs = DP / 16, kDt = DP / 32, kSub = BN / 32;
-    __shared__ __attribute__((aligned(16))) char lds[4 * Tile::kBytes];
+    __shared__ __attribute__((aligned(128))) char lds[4 * Tile::kBytes];
     __shared__ int range[2][NW];
     const AtShape &s = a.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), half = lane >> 5;
@@ -261,17 +261,21 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
 #pragma unroll
         for (int i = 0; i < 16; ++i) dq[d][i] = 0.0f;
 
-    auto work = [&](const char *lk, const char *lv, int j0, auto masked) __attribute__((always_inline)) {
+    const uint32_t plain_at = at_address(lds) + at_plain_lane<DP>(lane), trans_at = at_address(lds) + at_trans_lane<DP>(lane);
+    auto work = [&](int cur, int j0, auto masked) __attribute__((always_inline)) {
         constexpr bool kMasked = decltype(masked)::value;
+        const uint32_t ka = plain_at + cur * 2 * Tile::kBytes, va = ka + Tile::kBytes, kt = trans_at + cur * 2 * Tile::kBytes;
 #pragma unroll
         for (int t = 0; t < kSub; ++t) {
             at_acc x, y;
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = y[i] = 0.0f;
 #pragma unroll
-            for (int ks = 0; ks < kKs; ++ks) x = Num::mfma(at_plain<DP>(lk, t * 32, ks, lane), qf[ks], x);
-#pragma unroll
-            for (int ks = 0; ks < kKs; ++ks) y = Num::mfma(at_plain<DP>(lv, t * 32, ks, lane), gf[ks], y);
+            for (int ks = 0; ks < kKs; ++ks) {
+                x = Num::mfma(at_plain<DP>(ka, t * 32, ks), qf[ks], x);
+                y = Num::mfma(at_plain<DP>(va, t * 32, ks), gf[ks], y);
+                if (ks % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+            }
             const int first = j0 + t * 32 + 4 * half;
             const float away = BIAS ? float(place - first) : 0.0f;
             u32x4 ds[2], seen[2];
@@ -306,9 +310,10 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
             for (int g = 0; g < 2; ++g)
 #pragma unroll
                 for (int d = 0; d < kDt; ++d) {
-                    u32x4 f = at_transposed<DP>(lk, t * 32 + g * 16, d * 32, lane);
+                    u32x4 f = at_transposed<DP>(kt, t * 32 + g * 16, d * 32);
                     if (kMasked) f &= seen[g];
                     dq[d] = Num::mfma(f, ds[g], dq[d]);
+                    if (d == kDt - 1) __builtin_amdgcn_sched_barrier(0);
                 }
         }
     };
@@ -321,8 +326,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
         if (t + 1 < t1) fetch(t + 1);
         const int j0 = t * BN;
         if (j0 + BN <= wlo || j0 >= whi) continue;
-        if (j0 >= flo && j0 + BN <= fhi) work(lk, lv, j0, std::false_type());
-        else work(lk, lv, j0, std::true_type());
+        if (j0 >= flo && j0 + BN <= fhi) work(cur, j0, std::false_type());
+        else work(cur, j0, std::true_type());
     }
     if (r_own >= s.R) return;
     char *p = a.dq.p + int64_t(b) * a.dq.batch + int64_t(row.token) * a.dq.token + int64_t(hq) * a.dq.head;
@@ -346,7 +351,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
     typedef AtTile<256, kRows, DP> Tile;
     constexpr int kKs = DP / 16, kDt = DP / 32;
     constexpr int kInfo = BIAS ? 6 : 4;               // lse2, delta, lo, hi and, with a bias, slope and place
-    __shared__ __attribute__((aligned(16))) char lds[4 * Tile::kBytes];
+    __shared__ __attribute__((aligned(128))) char lds[4 * Tile::kBytes];
     __shared__ __attribute__((aligned(16))) uint32_t info[2][kInfo][kRows];
     const AtShape &s = a.s;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
@@ -449,15 +454,17 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
 #pragma unroll
         for (int i = 0; i < 16; ++i) dk[d][i] = dv[d][i] = 0.0f;
 
-    auto work = [&](const char *lq, const char *lg, const uint32_t (*in)[kRows], auto masked) __attribute__((always_inline)) {
+    const uint32_t plain_at = at_address(lds) + at_plain_lane<DP>(lane), trans_at = at_address(lds) + at_trans_lane<DP>(lane);
+    auto work = [&](int cur, const uint32_t (*in)[kRows], auto masked) __attribute__((always_inline)) {
         constexpr bool kMasked = decltype(masked)::value;
+        const uint32_t qa = plain_at + cur * 2 * Tile::kBytes, ga = qa + Tile::kBytes, qt = trans_at + cur * 2 * Tile::kBytes, gt = qt + Tile::kBytes;
         at_acc x, y;
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = y[i] = 0.0f;
 #pragma unroll
-        for (int ks = 0; ks < kKs; ++ks) x = Num::mfma(at_plain<DP>(lq, 0, ks, lane), kf[ks], x);
+        for (int ks = 0; ks < kKs; ++ks) x = Num::mfma(at_plain<DP>(qa, 0, ks), kf[ks], x);
 #pragma unroll
-        for (int ks = 0; ks < kKs; ++ks) y = Num::mfma(at_plain<DP>(lg, 0, ks, lane), vf[ks], y);
+        for (int ks = 0; ks < kKs; ++ks) y = Num::mfma(at_plain<DP>(ga, 0, ks), vf[ks], y);
         u32x4 p[2], ds[2], seen[2];
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
@@ -509,10 +516,10 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
         for (int g = 0; g < 2; ++g)
 #pragma unroll
             for (int d = 0; d < kDt; ++d) {
-                u32x4 f = at_transposed<DP>(lg, g * 16, d * 32, lane);
+                u32x4 f = at_transposed<DP>(gt, g * 16, d * 32);
                 if (kMasked) f &= seen[g];
                 dv[d] = Num::mfma(f, p[g], dv[d]);
-                u32x4 h = at_transposed<DP>(lq, g * 16, d * 32, lane);
+                u32x4 h = at_transposed<DP>(qt, g * 16, d * 32);
                 if (kMasked) h &= seen[g];
                 dk[d] = Num::mfma(h, ds[g], dk[d]);
             }
@@ -527,8 +534,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
         __syncthreads();
         const int after = __builtin_amdgcn_readfirstlane(next());
         if (after >= 0) fetch(after >> 1);
-        if (t & 1) work(lq, lg, info[cur], std::false_type());
-        else work(lq, lg, info[cur], std::true_type());
+        if (t & 1) work(cur, info[cur], std::false_type());
+        else work(cur, info[cur], std::true_type());
         t = after;
     }
     if (j_own >= s.Nk) return;

@@ -102,7 +102,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_fwd(const AtFwd a)
     typedef AtNum<T> Num;
     typedef AtTile<NW * 64, BN, DP> Tile;
     constexpr int kKs = DP / 16, kDt = DP / 32, kSub = BN / 32;
-    __shared__ __attribute__((aligned(16))) char lds[4 * Tile::kBytes];      // two tiles of k, two of v
+    __shared__ __attribute__((aligned(128))) char lds[4 * Tile::kBytes];      // two tiles of k, two of v
     __shared__ int range[2][NW];
     const AtShape &s = a.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), half = lane >> 5;
@@ -160,15 +160,20 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_fwd(const AtFwd a)
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     float m = kAtLow, l = 0.0f;
 
-    auto work = [&](const char *lk, const char *lv, int j0, auto masked) __attribute__((always_inline)) {
+    const uint32_t plain_at = at_address(lds) + at_plain_lane<DP>(lane), trans_at = at_address(lds) + at_trans_lane<DP>(lane);
+    auto work = [&](int cur, int j0, auto masked) __attribute__((always_inline)) {
         constexpr bool kMasked = decltype(masked)::value;
+        const uint32_t ka = plain_at + cur * 2 * Tile::kBytes, va = trans_at + cur * 2 * Tile::kBytes + Tile::kBytes;
         at_acc x[kSub];
 #pragma unroll
         for (int t = 0; t < kSub; ++t) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[t][i] = 0.0f;
 #pragma unroll
-            for (int ks = 0; ks < kKs; ++ks) x[t] = Num::mfma(at_plain<DP>(lk, t * 32, ks, lane), qf[ks], x[t]);
+            for (int ks = 0; ks < kKs; ++ks) {
+                x[t] = Num::mfma(at_plain<DP>(ka, t * 32, ks), qf[ks], x[t]);
+                if (ks % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
         }
         const int first = j0 + 4 * half;           // the key of register 0
         u32x4 seen[2 * kSub];
@@ -235,9 +240,10 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_fwd(const AtFwd a)
         for (int g = 0; g < 2 * kSub; ++g)
 #pragma unroll
             for (int d = 0; d < kDt; ++d) {
-                u32x4 f = at_transposed<DP>(lv, g * 16, d * 32, lane);
+                u32x4 f = at_transposed<DP>(va, g * 16, d * 32);
                 if (kMasked) f &= seen[g];
                 o[d] = Num::mfma(f, p[g], o[d]);
+                if (d == kDt - 1) __builtin_amdgcn_sched_barrier(0);
             }
     };
 
@@ -250,8 +256,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_fwd(const AtFwd a)
         if (t + 1 < t1) fetch(t + 1);
         const int j0 = t * BN;
         if (j0 + BN <= wlo || j0 >= whi) continue;
-        if (j0 >= flo && j0 + BN <= fhi) work(lk, lv, j0, std::false_type());
-        else work(lk, lv, j0, std::true_type());
+        if (j0 >= flo && j0 + BN <= fhi) work(cur, j0, std::false_type());
+        else work(cur, j0, std::true_type());
     }
 
     l = at_pair_sum(l);
