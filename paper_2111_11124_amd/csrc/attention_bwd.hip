@@ -21,20 +21,48 @@ constexpr int kAbRows = 128;           // rows of a workgroup of the row pass, a
 constexpr int kAbTile = 32;            // rows per step of the walk over rows
 constexpr int kAbKeys = 128;           // keys of a workgroup
 
-struct AbRows {                        // what the row pass leaves, [b * Hk + key head][padded rows]
-    float *lse2, *delta;               // log-sum-exp in powers of two; padded rows and rows that see nothing: 3e38, 0
-    int32_t *lo, *hi;                  // padded rows: 0, 0
-    int4 *tiles;                       // [..][tile]: least lo, largest hi of the rows that see something; largest lo, least hi of all
-    float2 *most;                      // [..][row block]: largest |do|, largest |delta|    (binary16 only)
-    float *values;                     // [..][128 keys]: largest |v|                       (binary16 only)
-    uint32_t rows, blocks, key_blocks; // padded rows (a multiple of 128), row blocks, blocks of 128 keys
+// The walk over rows takes them in tiles of 32 places: as many whole tokens of a group's G heads as fit, or 32 of one token's
+// heads where G is larger, so that a place's token and head within its tile are the same in every tile.
+struct AbOrder {
+    int32_t tokens, heads, parts;      // of a tile: tokens, heads; tiles per token (1 where a token fits)
+    uint32_t tiles;                    // of a (sequence, key head) pair; always even
+    FastDiv div_heads, div_parts;
 };
+enum { kAbLse = 0, kAbDelta, kAbLo, kAbHi, kAbSlope, kAbPlace, kAbEmpty, kAbWords };   // 32 words of each per tile
+struct AbRows {                        // what the row pass leaves
+    uint32_t *info;                    // [b * Hk + key head][tile][word][place]: log-sum-exp in powers of two (3e38 where nothing is seen), delta,
+                                       // interval, slope in powers of two, place of the query, 1 where nothing is seen
+    int4 *tiles;                       // [..][tile]: least lo, largest hi of the rows that see something; largest lo, least hi of all
+    float2 *most;                      // [..][four tiles]: largest |do|, largest |delta|   (binary16 only)
+    float *values;                     // [..][128 keys]: largest |v|                       (binary16 only)
+    uint32_t blocks, key_blocks;       // of four tiles, of 128 keys
+};
+struct AbPlace {
+    int64_t token;
+    int32_t g;
+    bool live;
+};
+__device__ __forceinline__ AbPlace ab_place(const AtShape &s, const AbOrder &w, uint32_t tile, int x)   // the row of a tile's place x
+{
+    const uint32_t t = w.parts == 1 ? tile : fastdiv(tile, w.div_parts), dt = fastdiv(uint32_t(x), w.div_heads);
+    AbPlace p;
+    p.token = int64_t(t) * w.tokens + dt;
+    p.g = int(tile - t * w.parts) * 32 + (x - int(dt) * w.heads);
+    p.live = int(dt) < w.tokens && p.token < s.Nq && p.g < s.G;
+    return p;
+}
+__device__ __forceinline__ int64_t ab_info(const AbOrder &w, uint32_t head, uint32_t token, uint32_t g)   // where a row's words are
+{
+    const uint32_t t = token / uint32_t(w.tokens), x = (token - t * w.tokens) * w.heads + (g & 31u);
+    return (int64_t(head) * w.tiles + t * w.parts + (w.parts == 1 ? 0 : g >> 5)) * (kAbWords * 32) + (w.parts == 1 ? (token - t * w.tokens) * w.heads + g : x);
+}
 struct AtBwd {
     AtShape s;
     AtView q, k, v, o, dO;
     AtOut dq, dk, dv;
     const float *lse;
     AbRows w;
+    AbOrder order;
     float *part;                       // [split][b * Hk + head][Nk][2][D]; null: no split
     uint32_t heads, key_blocks, splits, row_blocks;
 };
@@ -61,7 +89,7 @@ __global__ __launch_bounds__(kThreads) void k_attn_operand(AtView q, const float
     Store<T>::store(out, row * D + e, Store<T>::pack(f));
 }
 
-// The row pass.  Workgroups [0, blocks) of a head: 128 rows' deltas, log-sum-exps, intervals and the summaries of their four
+// The row pass.  Workgroups [0, blocks) of a head: the deltas of 128 places, log-sum-exps, intervals and the summaries of their four
 // tiles; further ones (binary16): the largest norm of 128 keys' values.  Eight or sixteen lanes per row.
 template <typename T, int DP>
 __global__ __launch_bounds__(kThreads) void k_attn_rows(const AtBwd a)
@@ -90,46 +118,53 @@ __global__ __launch_bounds__(kThreads) void k_attn_rows(const AtBwd a)
     } else {
         __shared__ uint32_t empty[kAbRows / 32];
         if (tid < kAbRows) {
-            const uint32_t r = blk * kAbRows + tid;
-            int lo = 0, hi = 0;
-            float lse2 = 3.0e38f;
-            if (r < s.R) {
-                const AtRow row = at_row(s, r);
-                at_interval(s, b, row.token, lo, hi);
+            const uint32_t tile = blk * 4 + (tid >> 5);
+            const int x = tid & 31;
+            const AbPlace row = ab_place(s, a.order, tile, x);
+            int lo = 0, hi = 0, place = 0;
+            float lse2 = 3.0e38f, slope2 = 0.0f;
+            if (row.live) {
+                at_interval(s, b, uint32_t(row.token), lo, hi);
                 if (hi > 0) {
-                    lse2 = a.lse[(int64_t(b) * s.Hq + hk * s.G + int(row.g)) * s.Nq + row.token] * kLog2e;
+                    lse2 = a.lse[(int64_t(b) * s.Hq + hk * s.G + row.g) * s.Nq + row.token] * kLog2e;
                     if (AtNum<T>::kHalf) lse2 -= float(kAtDrop);
                 }
+                place = at_place(s, b, uint32_t(row.token));
+                if (s.slopes) slope2 = s.slopes[hk * s.G + row.g] * kLog2e;
             }
-            const int64_t at = int64_t(head) * a.w.rows + r;
-            a.w.lse2[at] = lse2;
-            a.w.lo[at] = lo;
-            a.w.hi[at] = hi;
             const uint64_t none = __ballot(hi == 0);
             int l0 = hi > 0 ? lo : 0x7FFFFFFF, h1 = hi, l1 = lo, h0 = hi;
 #pragma unroll
             for (int m = 1; m < 32; m <<= 1) {
-                int x = __shfl_xor(l0, m, 64); l0 = x < l0 ? x : l0;
-                x = __shfl_xor(h1, m, 64); h1 = x > h1 ? x : h1;
-                x = __shfl_xor(l1, m, 64); l1 = x > l1 ? x : l1;
-                x = __shfl_xor(h0, m, 64); h0 = x < h0 ? x : h0;
+                int y = __shfl_xor(l0, m, 64); l0 = y < l0 ? y : l0;
+                y = __shfl_xor(h1, m, 64); h1 = y > h1 ? y : h1;
+                y = __shfl_xor(l1, m, 64); l1 = y > l1 ? y : l1;
+                y = __shfl_xor(h0, m, 64); h0 = y < h0 ? y : h0;
             }
-            if ((tid & 31) == 0) {
-                a.w.tiles[(int64_t(head) * a.w.rows + r) / 32] = make_int4(l0, h1, l1, h0);
-                empty[tid >> 5] = uint32_t(none >> (tid & 32));
+            if (tile < a.order.tiles) {
+                const int64_t at = int64_t(head) * a.order.tiles + tile;
+                uint32_t *p = a.w.info + at * (kAbWords * 32) + x;
+                p[kAbLse * 32] = __float_as_uint(lse2);
+                p[kAbLo * 32] = uint32_t(lo);
+                p[kAbHi * 32] = uint32_t(hi);
+                p[kAbSlope * 32] = __float_as_uint(slope2);
+                p[kAbPlace * 32] = uint32_t(place);
+                p[kAbEmpty * 32] = hi == 0;
+                if (x == 0) a.w.tiles[at] = make_int4(l0, h1, l1, h0);
             }
+            if (x == 0) empty[tid >> 5] = uint32_t(none >> (tid & 32));
         }
         __syncthreads();
-        for (int x = first; x < kAbRows; x += kPer) {
-            const uint32_t r = blk * kAbRows + x;
-            const bool live = r < s.R && !(empty[x >> 5] >> (x & 31) & 1u);
+        for (int y = first; y < kAbRows; y += kPer) {
+            const uint32_t tile = blk * 4 + (y >> 5);
+            const AbPlace row = ab_place(s, a.order, tile, y & 31);
+            const bool live = row.live && !(empty[y >> 5] >> (y & 31) & 1u);
             float dot = 0.0f, ss = 0.0f;
             if (live && part * 8 < s.D) {
-                const AtRow row = at_row(s, r);
-                const int64_t h = hk * s.G + int64_t(row.g);
+                const int64_t h = hk * s.G + row.g;
                 float f[8], g[8];
-                Store<T>::unpack(Store<T>::load(a.o.p + int64_t(b) * a.o.batch + int64_t(row.token) * a.o.token + h * a.o.head, part * 8), f);
-                Store<T>::unpack(Store<T>::load(a.dO.p + int64_t(b) * a.dO.batch + int64_t(row.token) * a.dO.token + h * a.dO.head, part * 8), g);
+                Store<T>::unpack(Store<T>::load(a.o.p + int64_t(b) * a.o.batch + row.token * a.o.token + h * a.o.head, part * 8), f);
+                Store<T>::unpack(Store<T>::load(a.dO.p + int64_t(b) * a.dO.batch + row.token * a.dO.token + h * a.dO.head, part * 8), g);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     dot = fmaf(f[k], g[k], dot);
@@ -137,7 +172,7 @@ __global__ __launch_bounds__(kThreads) void k_attn_rows(const AtBwd a)
                 }
             }
             dot = lanes_sum_dpp<kLanes>(dot);
-            if (part == 0) a.w.delta[int64_t(head) * a.w.rows + r] = dot;
+            if (part == 0 && tile < a.order.tiles) a.w.info[(int64_t(head) * a.order.tiles + tile) * (kAbWords * 32) + kAbDelta * 32 + (y & 31)] = __float_as_uint(dot);
             if (AtNum<T>::kHalf) {
                 most = fmaxf(most, lanes_sum_dpp<kLanes>(ss));
                 most_delta = fmaxf(most_delta, fabsf(dot));
@@ -202,9 +237,9 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
     const uint32_t r_own = (rb * NW + wave) * 32 + (lane & 31), r = r_own < s.R ? r_own : s.R - 1;
     const AtRow row = at_row(s, r);
     const int hq = hk * s.G + int(row.g);
-    const int64_t at = int64_t(head) * a.w.rows + r;
-    const int lo = a.w.lo[at], hi = a.w.hi[at];
-    const float lse2 = a.w.lse2[at], delta = a.w.delta[at];
+    const uint32_t *info = a.w.info + ab_info(a.order, head, row.token, row.g);
+    const int lo = int(info[kAbLo * 32]), hi = int(info[kAbHi * 32]);
+    const float lse2 = __uint_as_float(info[kAbLse * 32]), delta = __uint_as_float(info[kAbDelta * 32]);
     const int wlo = at_wave_min(hi > 0 ? lo : 0x7FFFFFFF), whi = at_wave_max(hi), flo = at_wave_max(lo), fhi = at_wave_min(hi);
     if (lane == 0) {
         range[0][wave] = wlo;
@@ -343,21 +378,24 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
 // ---------------------------------------------------------------------------------------------
 // dk, dv: a wave owns 32 keys
 // ---------------------------------------------------------------------------------------------
+// A step is two tiles of 32 rows.  Where a tile lies at the edge of what its rows see, probabilities are set to zero element by
+// element; rows that see nothing are zeros in LDS, so that what they hold does not enter.
 template <typename T, int DP, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd a)
 {
     typedef AtNum<T> Num;
-    constexpr int kRows = kAbTile;
-    typedef AtTile<256, kRows, DP> Tile;
-    constexpr int kKs = DP / 16, kDt = DP / 32;
-    constexpr int kInfo = BIAS ? 6 : 4;               // lse2, delta, lo, hi and, with a bias, slope and place
-    __shared__ __attribute__((aligned(128))) char lds[4 * Tile::kBytes];
-    __shared__ __attribute__((aligned(16))) uint32_t info[2][kInfo][kRows];
+    constexpr int kKs = DP / 16, kDt = DP / 32, kPieces = DP / 8;
+    constexpr int kTile = kAbTile * DP * 2;           // bytes: 32 rows of q, or of do
+    constexpr int kOff = kAbTile * kPieces / 256;     // rows of a tile per thread
+    constexpr int kInfo = BIAS ? 6 : 4;               // words per row that are used here
+    __shared__ __attribute__((aligned(128))) char lds[2 * 4 * kTile];          // [buffer][tile][q, do]
+    __shared__ __attribute__((aligned(16))) uint32_t info[2][2][kInfo * 32];   // [buffer][tile][word][row]
     const AtShape &s = a.s;
+    const AbOrder &order = a.order;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     const uint32_t head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, split = rest % a.splits, kb = rest / a.splits;   // the keys that most rows see first
     const int b = int(head / uint32_t(s.Hk)), hk = int(head) - b * s.Hk;
-    const int k0 = int(kb) * kAbKeys, j_own = k0 + wave * 32 + (lane & 31), j = j_own < s.Nk ? j_own : s.Nk - 1;
+    const int k0 = int(kb) * kAbKeys, j0 = k0 + wave * 32, j_own = j0 + (lane & 31), j = j_own < s.Nk ? j_own : s.Nk - 1;
     u32x4 kf[kKs], vf[kKs];
     {
         const char *p = a.k.p + int64_t(b) * a.k.batch + int64_t(j) * a.k.token + int64_t(hk) * a.k.head;
@@ -395,58 +433,76 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
         undo_v = ab_pow2(-kAtDrop);
     }
     const char *qbase = a.q.p + int64_t(b) * a.q.batch + int64_t(hk) * s.G * a.q.head, *gbase = a.dO.p + int64_t(b) * a.dO.batch + int64_t(hk) * s.G * a.dO.head;
-    const int64_t info_at = int64_t(head) * a.w.rows;
-    const int4 *tiles = a.w.tiles + info_at / 32;
-    const int count = int((s.R + kRows - 1) / kRows);       // tiles of rows; this workgroup's: split, split + splits, ...
-    const int mine = (count - int(split) + int(a.splits) - 1) / int(a.splits);
+    const int4 *tiles = a.w.tiles + int64_t(head) * order.tiles;
+    const uint32_t *words = a.w.info + int64_t(head) * order.tiles * (kAbWords * 32);
+    const int pairs = int(order.tiles / 2), mine = (pairs - int(split) + int(a.splits) - 1) / int(a.splits);   // this workgroup's: split, split + splits, ...
 
-    // the next tile that this workgroup's keys meet: 64 summaries at a time, one per lane
+    // this thread's pieces of a tile: the rows' places within it
+    uint32_t q_at[kOff], g_at[kOff], lds_at[kOff], empty_at[kOff];
+    int dt[kOff], dg[kOff];
+    const int piece = tid % kPieces;
+#pragma unroll
+    for (int k = 0; k < kOff; ++k) {
+        const int x = tid / kPieces + k * (256 / kPieces);
+        dt[k] = int(fastdiv(uint32_t(x), order.div_heads));
+        dg[k] = x - dt[k] * order.heads;
+        const bool in = dt[k] < order.tokens && piece * 8 < s.D;
+        q_at[k] = uint32_t(dt[k]) * uint32_t(a.q.token) + uint32_t(dg[k]) * uint32_t(a.q.head) + piece * 16;
+        g_at[k] = uint32_t(dt[k]) * uint32_t(a.dO.token) + uint32_t(dg[k]) * uint32_t(a.dO.head) + piece * 16;
+        lds_at[k] = x * (DP * 2) + ((piece ^ at_turn(x)) << 4);
+        empty_at[k] = (kAbEmpty * 32 + x) * 4;
+        if (!in) dt[k] = 0x40000000;
+    }
+
+    // the next pair of tiles that this workgroup's keys meet: 64 summaries at a time, one per lane; what each wave makes of them
     int base = -64;
-    uint64_t meets = 0, whole = 0;
+    uint64_t meets = 0, mine0 = 0, mine1 = 0, whole0 = 0, whole1 = 0, some = 0;
     auto next = [&]() __attribute__((always_inline)) {
         while (meets == 0) {
             base += 64;
             if (base >= mine) return -1;
             const int n = base + lane;
-            bool in = false, all = false;
+            int4 t[2] = {make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
             if (n < mine) {
-                const int4 t = tiles[int(split) + n * int(a.splits)];
-                in = t.y > k0 && t.x < k0 + kAbKeys;
-                all = t.w >= k0 + kAbKeys && t.z <= k0;
+                const int4 *p = tiles + 2 * (int(split) + n * int(a.splits));
+                t[0] = p[0];
+                t[1] = p[1];
             }
-            meets = __ballot(in);
-            whole = __ballot(all);
+            meets = __ballot((t[0].y > k0 && t[0].x < k0 + kAbKeys) || (t[1].y > k0 && t[1].x < k0 + kAbKeys));
+            mine0 = __ballot(t[0].y > j0 && t[0].x < j0 + 32);
+            mine1 = __ballot(t[1].y > j0 && t[1].x < j0 + 32);
+            whole0 = __ballot(t[0].w >= j0 + 32 && t[0].z <= j0);
+            whole1 = __ballot(t[1].w >= j0 + 32 && t[1].z <= j0);
+            some = __ballot(t[0].w == 0 || t[1].w == 0);
         }
         const int bit = __builtin_ctzll(meets);
         meets &= meets - 1;
-        return ((int(split) + (base + bit) * int(a.splits)) << 1) | int(whole >> bit & 1u);
+        return ((int(split) + (base + bit) * int(a.splits)) << 5) | int(mine0 >> bit & 1u) | int(mine1 >> bit & 1u) << 1 | int(whole0 >> bit & 1u) << 2 | int(whole1 >> bit & 1u) << 3 |
+               int(some >> bit & 1u) << 4;
     };
-    Tile tq, tg;
-    uint32_t word = 0;
-    auto fetch = [&](int t) __attribute__((always_inline)) {
-        const uint32_t r0 = uint32_t(t) * kRows;
-        const AtRow first = at_row(s, r0);
-        const int left = int(s.R - r0 < kRows ? s.R - r0 : kRows);
-        // a row's place from the first row's token
-        auto off = [&](int64_t token, int64_t headstep, int x) __attribute__((always_inline)) {
-            if (s.G == 1) return uint32_t(x * int(token));
-            const uint32_t u = first.g + uint32_t(x), n = fastdiv(u, s.div_g);
-            return n * uint32_t(token) + (u - n * uint32_t(s.G)) * uint32_t(headstep);
-        };
-        tq.load(qbase + int64_t(first.token) * a.q.token, left, s.D, [&](int x) { return off(a.q.token, a.q.head, x); });
-        tg.load(gbase + int64_t(first.token) * a.dO.token, left, s.D, [&](int x) { return off(a.dO.token, a.dO.head, x); });
-        if (tid < kInfo * kRows) {
-            const int what = tid / kRows, x = tid % kRows;
-            const int64_t at = info_at + r0 + x;
-            if (what == 0) word = __float_as_uint(a.w.lse2[at]);
-            else if (what == 1) word = __float_as_uint(a.w.delta[at]);
-            else if (what == 2) word = uint32_t(a.w.lo[at]);
-            else if (what == 3) word = uint32_t(a.w.hi[at]);
-            else if (BIAS) {
-                const AtRow row = at_row(s, r0 + x < s.R ? r0 + x : s.R - 1);
-                word = what == 4 ? __float_as_uint(s.slopes[hk * s.G + int(row.g)] * kLog2e) : uint32_t(at_place(s, b, row.token));
+    u32x4 tq[2][kOff], tg[2][kOff];
+    uint32_t dead[2][kOff], word, word2 = 0;
+    auto fetch = [&](int what) __attribute__((always_inline)) {
+        const bool check = what & 16;                  // some row of these tiles sees nothing
+        const uint32_t pair = uint32_t(what >> 5);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint32_t tile = pair * 2 + u, t = order.parts == 1 ? tile : fastdiv(tile, order.div_parts);
+            const int64_t token = int64_t(t) * order.tokens;
+            const int g0 = int(tile - t * order.parts) * 32, left = int(s.Nq - token < 64 ? s.Nq - token : 64), heads = s.G - g0;
+            const Span q(qbase + token * a.q.token + int64_t(g0) * a.q.head, kNowhere), g(gbase + token * a.dO.token + int64_t(g0) * a.dO.head, kNowhere);
+            const Span e(words + int64_t(tile) * (kAbWords * 32), check ? kAbWords * 128 : 0);
+#pragma unroll
+            for (int k = 0; k < kOff; ++k) {
+                const bool in = dt[k] < left && dg[k] < heads;
+                q.load_kept(in ? q_at[k] : kNowhere, tq[u][k]);
+                g.load_kept(in ? g_at[k] : kNowhere, tg[u][k]);
+                dead[u][k] = __float_as_uint(e.load_f32(empty_at[k]));   // zero where nothing is to be checked
             }
         }
+        const uint32_t *p = words + int64_t(pair) * 2 * (kAbWords * 32);
+        word = p[(tid >> 7) * (kAbWords * 32) + (tid & 127)];
+        if (BIAS) word2 = p[((tid >> 6) & 1) * (kAbWords * 32) + 128 + (tid & 63)];
     };
     at_acc dk[kDt], dv[kDt];
 #pragma unroll
@@ -455,9 +511,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
         for (int i = 0; i < 16; ++i) dk[d][i] = dv[d][i] = 0.0f;
 
     const uint32_t plain_at = at_address(lds) + at_plain_lane<DP>(lane), trans_at = at_address(lds) + at_trans_lane<DP>(lane);
-    auto work = [&](int cur, const uint32_t (*in)[kRows], auto masked) __attribute__((always_inline)) {
-        constexpr bool kMasked = decltype(masked)::value;
-        const uint32_t qa = plain_at + cur * 2 * Tile::kBytes, ga = qa + Tile::kBytes, qt = trans_at + cur * 2 * Tile::kBytes, gt = qt + Tile::kBytes;
+    auto work = [&](int at, const uint32_t *in, bool whole) __attribute__((always_inline)) {
+        const uint32_t qa = plain_at + at, ga = qa + kTile, qt = trans_at + at, gt = qt + kTile;
         at_acc x, y;
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = y[i] = 0.0f;
@@ -465,77 +520,80 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
         for (int ks = 0; ks < kKs; ++ks) x = Num::mfma(at_plain<DP>(qa, 0, ks), kf[ks], x);
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks) y = Num::mfma(at_plain<DP>(ga, 0, ks), vf[ks], y);
-        u32x4 p[2], ds[2], seen[2];
+        auto row4 = [&](int word, int w) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4 *>(in + word * 32 + 8 * w + 4 * half); };   // rows of registers 4w..4w+3
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            bool vis[8];
-            float pe[8], z[8];
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                const int at = 8 * (2 * g + w) + 4 * half;         // rows of four registers
-                const u32x4 l4 = *reinterpret_cast<const u32x4 *>(&in[0][at]), d4 = *reinterpret_cast<const u32x4 *>(&in[1][at]);
-                u32x4 lo4 = {}, hi4 = {}, sl4 = {}, pl4 = {};
-                if (kMasked) {
-                    lo4 = *reinterpret_cast<const u32x4 *>(&in[2][at]);
-                    hi4 = *reinterpret_cast<const u32x4 *>(&in[3][at]);
-                }
-                if (BIAS) {
-                    sl4 = *reinterpret_cast<const u32x4 *>(&in[kInfo - 2][at]);
-                    pl4 = *reinterpret_cast<const u32x4 *>(&in[kInfo - 1][at]);
-                }
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int e = 4 * w + c, i = 8 * g + e;
-                    const float lse2 = __uint_as_float(l4[c]);
-                    float slope = 1.0f;
-                    if (!CAP && !BIAS) {
-                        pe[e] = at_exp2(fmaf(x[i], s.c, -lse2));
-                    } else {
-                        float sc = ab_score<CAP>(s, x[i], slope);
-                        if (BIAS) sc = fmaf(-__uint_as_float(sl4[c]), fabsf(float(int(pl4[c]) - j_own)), sc);
-                        pe[e] = at_exp2(sc - lse2);
-                    }
-                    z[e] = pe[e] * (y[i] - __uint_as_float(d4[c]));
-                    if (CAP) z[e] *= slope;
-                    if (Num::kHalf) z[e] *= mul;
-                    if (kMasked) {
-                        vis[e] = j_own >= int(lo4[c]) && j_own < int(hi4[c]);
-                        pe[e] = vis[e] ? pe[e] : 0.0f;
-                        z[e] = vis[e] ? z[e] : 0.0f;
-                    }
-                }
+        for (int w = 0; w < 4; ++w) {
+            const u32x4 l4 = row4(kAbLse, w), d4 = row4(kAbDelta, w);
+            u32x4 sl4 = {}, pl4 = {};
+            if (BIAS) {
+                sl4 = row4(kAbSlope, w);
+                pl4 = row4(kAbPlace, w);
             }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int i = 4 * w + c;
+                const float lse2 = __uint_as_float(l4[c]);
+                float slope = 1.0f;
+                if (!CAP && !BIAS) {
+                    x[i] = at_exp2(fmaf(x[i], s.c, -lse2));
+                } else {
+                    float sc = ab_score<CAP>(s, x[i], slope);
+                    if (BIAS) sc = fmaf(-__uint_as_float(sl4[c]), fabsf(float(int(pl4[c]) - j_own)), sc);
+                    x[i] = at_exp2(sc - lse2);
+                }
+                y[i] = x[i] * (y[i] - __uint_as_float(d4[c]));
+                if (CAP) y[i] *= slope;
+                if (Num::kHalf) y[i] *= mul;
+            }
+        }
+        if (!whole) {
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                p[g][w] = Num::pack(pe[2 * w], pe[2 * w + 1]);
-                ds[g][w] = Num::pack(z[2 * w], z[2 * w + 1]);
+                const u32x4 lo4 = row4(kAbLo, w), hi4 = row4(kAbHi, w);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const bool vis = uint32_t(j_own - int(lo4[c])) < hi4[c] - lo4[c];
+                    x[4 * w + c] = vis ? x[4 * w + c] : 0.0f;
+                    y[4 * w + c] = vis ? y[4 * w + c] : 0.0f;
+                }
             }
-            if (kMasked) seen[g] = at_seen(vis, lane);
         }
+        u32x4 p[2], ds[2];
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                p[g][w] = Num::pack(x[8 * g + 2 * w], x[8 * g + 2 * w + 1]);
+                ds[g][w] = Num::pack(y[8 * g + 2 * w], y[8 * g + 2 * w + 1]);
+            }
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
             for (int d = 0; d < kDt; ++d) {
-                u32x4 f = at_transposed<DP>(gt, g * 16, d * 32);
-                if (kMasked) f &= seen[g];
-                dv[d] = Num::mfma(f, p[g], dv[d]);
-                u32x4 h = at_transposed<DP>(qt, g * 16, d * 32);
-                if (kMasked) h &= seen[g];
-                dk[d] = Num::mfma(h, ds[g], dk[d]);
+                dv[d] = Num::mfma(at_transposed<DP>(gt, g * 16, d * 32), p[g], dv[d]);
+                dk[d] = Num::mfma(at_transposed<DP>(qt, g * 16, d * 32), ds[g], dk[d]);
             }
     };
     int t = __builtin_amdgcn_readfirstlane(next());
-    if (t >= 0) fetch(t >> 1);
+    if (t >= 0) fetch(t);
     for (int cur = 0; t >= 0; cur ^= 1) {
-        char *lq = lds + cur * 2 * Tile::kBytes, *lg = lq + Tile::kBytes;
-        tq.store(lq);
-        tg.store(lg);
-        if (tid < kInfo * kRows) info[cur][tid / kRows][tid % kRows] = word;
+        char *p = lds + cur * 4 * kTile;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int k = 0; k < kOff; ++k) {
+                const u32x4 keep = dead[u][k] ? u32x4{0u, 0u, 0u, 0u} : u32x4{~0u, ~0u, ~0u, ~0u};
+                *reinterpret_cast<u32x4 *>(p + u * 2 * kTile + lds_at[k]) = tq[u][k] & keep;
+                *reinterpret_cast<u32x4 *>(p + u * 2 * kTile + kTile + lds_at[k]) = tg[u][k] & keep;
+            }
+        info[cur][tid >> 7][tid & 127] = word;
+        if (BIAS && tid < 128) info[cur][tid >> 6][(128 + (tid & 63)) % (kInfo * 32)] = word2;
         __syncthreads();
         const int after = __builtin_amdgcn_readfirstlane(next());
-        if (after >= 0) fetch(after >> 1);
-        if (t & 1) work(cur, info[cur], std::false_type());
-        else work(cur, info[cur], std::true_type());
+        if (after >= 0) fetch(after);
+#pragma unroll 1
+        for (int u = 0; u < 2; ++u)
+            if (t >> u & 1) work(cur * 4 * kTile + u * 2 * kTile, info[cur][u], t >> (2 + u) & 1);
         t = after;
     }
     if (j_own >= s.Nk) return;
@@ -604,7 +662,8 @@ __global__ __launch_bounds__(kThreads) void k_attn_zero(AtOut o, int heads, int 
 }
 
 struct AtBwdPlan {
-    uint32_t rows, blocks, key_blocks, splits, row_blocks;
+    AbOrder order;
+    uint32_t blocks, key_blocks, splits, row_blocks;
     size_t info, part, operand[3], total;       // bytes
 };
 static size_t ab_up(size_t n) { return (n + 255) & ~size_t(255); }
@@ -612,18 +671,26 @@ static AtBwdPlan at_bwd_plan(const mesa_attention &a, const bool codes[3])
 {
     AtBwdPlan p;
     const int64_t R = a.Nq * (a.Hq / a.Hk), heads = a.B * a.Hk;
-    p.blocks = uint32_t(ceil_div(R, kAbRows));
-    p.rows = p.blocks * kAbRows;
+    const int64_t G = a.Hq / a.Hk;
+    AbOrder &o = p.order;
+    o.heads = int32_t(G > 32 ? 32 : G);
+    o.tokens = int32_t(G > 32 ? 1 : 32 / G);
+    o.parts = int32_t(ceil_div(G, 32));
+    const int64_t tiles = ceil_div(a.Nq, o.tokens) * o.parts;
+    o.tiles = uint32_t(tiles + (tiles & 1));
+    o.div_heads = make_fastdiv(uint32_t(o.heads));
+    o.div_parts = make_fastdiv(uint32_t(o.parts));
+    p.blocks = uint32_t(ceil_div(o.tiles, 4));
     p.key_blocks = uint32_t(ceil_div(a.Nk, kAbKeys));
     p.row_blocks = uint32_t(ceil_div(R, 128));
     // few keys and long walks: the rows' tiles are dealt out to several workgroups and their sums added up
-    const int64_t have = heads * p.key_blocks, most = R / (8 * kAbTile);
-    int64_t n = have > 0 ? 512 / have : 1;
+    const int64_t have = heads * p.key_blocks, most = o.tiles / 16;
+    int64_t n = have > 0 ? 1024 / have : 1;
     n = n > most ? most : n;
     n = n > 32 ? 32 : n < 1 ? 1 : n;
     p.splits = uint32_t(n);
     const size_t h = size_t(heads);
-    p.info = ab_up(h * p.rows * 4) * 4 + ab_up(h * p.rows / 32 * sizeof(int4)) + ab_up(h * p.blocks * sizeof(float2)) + ab_up(h * p.key_blocks * sizeof(float));
+    p.info = ab_up(h * o.tiles * kAbWords * 128) + ab_up(h * o.tiles * sizeof(int4)) + ab_up(h * p.blocks * sizeof(float2)) + ab_up(h * p.key_blocks * sizeof(float));
     p.part = n > 1 ? ab_up(size_t(n) * h * size_t(a.Nk) * 2 * size_t(a.D) * sizeof(float)) : 0;
     const int64_t tokens[3] = {a.Nq, a.Nk, a.Nk}, hs[3] = {a.Hq, a.Hk, a.Hk};
     p.total = p.info + p.part;
@@ -743,15 +810,12 @@ extern "C" MESA_EXPORT mesa_status mesa_attention_bwd_q(mesa_attention a, mesa_a
     f.splits = p.splits;
     f.row_blocks = p.row_blocks;
     char *w = static_cast<char *>(ws);
-    const size_t h = size_t(heads), line = ab_up(h * p.rows * 4);
-    f.w.lse2 = reinterpret_cast<float *>(w);
-    f.w.delta = reinterpret_cast<float *>(w + line);
-    f.w.lo = reinterpret_cast<int32_t *>(w + 2 * line);
-    f.w.hi = reinterpret_cast<int32_t *>(w + 3 * line);
-    f.w.tiles = reinterpret_cast<int4 *>(w + 4 * line);
-    f.w.most = reinterpret_cast<float2 *>(w + 4 * line + ab_up(h * p.rows / 32 * sizeof(int4)));
-    f.w.values = reinterpret_cast<float *>(w + 4 * line + ab_up(h * p.rows / 32 * sizeof(int4)) + ab_up(h * p.blocks * sizeof(float2)));
-    f.w.rows = p.rows;
+    const size_t h = size_t(heads), tiles_at = ab_up(h * p.order.tiles * kAbWords * 128), most_at = tiles_at + ab_up(h * p.order.tiles * sizeof(int4));
+    f.order = p.order;
+    f.w.info = reinterpret_cast<uint32_t *>(w);
+    f.w.tiles = reinterpret_cast<int4 *>(w + tiles_at);
+    f.w.most = reinterpret_cast<float2 *>(w + most_at);
+    f.w.values = reinterpret_cast<float *>(w + most_at + ab_up(h * p.blocks * sizeof(float2)));
     f.w.blocks = p.blocks;
     f.w.key_blocks = p.key_blocks;
     f.part = p.splits > 1 ? reinterpret_cast<float *>(w + p.info) : nullptr;
