@@ -127,6 +127,12 @@ template <int NT, int ROWS, int DP> struct AtTile {
             s.load_kept(row < rows && piece * 8 < D ? uint32_t(at(row)) + piece * 16 : kNowhere, r[k]);
         }
     }
+    __device__ __forceinline__ void keep(uint64_t rows)      // rows without a bit become zeros
+    {
+#pragma unroll
+        for (int k = 0; k < kN; ++k)
+            if (!(rows >> ((int(threadIdx.x) + k * NT) / kPieces) & 1u)) r[k] = u32x4{0u, 0u, 0u, 0u};
+    }
     __device__ __forceinline__ void store(char *lds) const
     {
 #pragma unroll
@@ -202,23 +208,25 @@ __device__ __forceinline__ float at_tanh(float u) { return fmaf(-2.0f, __builtin
 // index within a 32-row accumulator tile of register i, without the lane's part 4*(lane/32)
 __device__ __forceinline__ constexpr int at_reg_row(int i) { return 8 * (i / 4) + i % 4; }
 
-// Eight accumulator registers' worth of "some column of this wave's sees it": bits as AND masks for the A operand of the product
-// that contracts this index, so that what no column sees (padding; infinities and NaN there) enters as zero and
-// not as 0 * NaN.  vis[e]: this lane's column sees index e of its half.
-__device__ __forceinline__ u32x4 at_seen(const bool vis[8], int lane)
+// Tiles of keys at the edge of what a workgroup's rows see: keys that none of them sees are stored as zeros, so that what they hold
+// (padding; infinities and NaN there) enters no product as 0 * NaN.  lo, hi: this lane's row; the waves' answers meet in `seen`.
+// A bit per key of the tile; ends in a barrier's worth of order, so every wave of the workgroup has to come.
+template <int NW> __device__ __forceinline__ uint64_t at_seen(uint64_t *seen, int wave, int lane, int j0, int lo, int hi)
 {
-    u32x4 m;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        uint32_t word = 0u;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const uint64_t any = __ballot(vis[2 * w + k]);
-            const bool seen = lane < 32 ? uint32_t(any) != 0u : uint32_t(any >> 32) != 0u;
-            word |= seen ? (k ? 0xFFFF0000u : 0x0000FFFFu) : 0u;
-        }
-        m[w] = word;
+    bool any = false;
+#pragma unroll 8
+    for (int i = 0; i < 32; ++i) {
+        const int l = __builtin_amdgcn_readlane(lo, i), h = __builtin_amdgcn_readlane(hi, i);
+        any |= uint32_t(j0 + lane - l) < uint32_t(h - l);
     }
+    uint64_t m = __ballot(any);
+    if (NW == 1) return m;
+    __syncthreads();                               // the last answers have been read
+    if (lane == 0) seen[wave] = m;
+    __syncthreads();
+    m = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) m |= seen[w];
     return m;
 }
 

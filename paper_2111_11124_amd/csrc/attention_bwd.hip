@@ -229,7 +229,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
     typedef AtTile<NW * 64, BN, DP> Tile;
     constexpr int kKs = DP / 16, kDt = DP / 32, kSub = BN / 32;
     __shared__ __attribute__((aligned(128))) char lds[4 * Tile::kBytes];
-    __shared__ int range[2][NW];
+    __shared__ int range[4][NW];
+    __shared__ uint64_t seen[NW];
     const AtShape &s = a.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), half = lane >> 5;
     const uint32_t head = blockIdx.x % a.heads, rb = a.row_blocks - 1 - blockIdx.x / a.heads;
@@ -244,6 +245,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
     if (lane == 0) {
         range[0][wave] = wlo;
         range[1][wave] = whi;
+        range[2][wave] = flo;
+        range[3][wave] = fhi;
     }
     u32x4 qf[kKs], gf[kKs];
     {
@@ -258,12 +261,16 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
     const float slope2 = BIAS ? s.slopes[hq] * kLog2e : 0.0f;
     const int place = BIAS ? at_place(s, b, row.token) : 0;
     __syncthreads();
-    int blo = 0x7FFFFFFF, bhi = 0;
+    int blo = 0x7FFFFFFF, bhi = 0, all_lo = 0, all_hi = 0x7FFFFFFF;      // the same of the workgroup's rows
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
         blo = range[0][w] < blo ? range[0][w] : blo;
         bhi = range[1][w] > bhi ? range[1][w] : bhi;
+        all_lo = range[2][w] > all_lo ? range[2][w] : all_lo;
+        all_hi = range[3][w] < all_hi ? range[3][w] : all_hi;
     }
+    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+    all_hi = __builtin_amdgcn_readfirstlane(all_hi);
     const int t0 = __builtin_amdgcn_readfirstlane(bhi > 0 ? blo / BN : 0), t1 = __builtin_amdgcn_readfirstlane(bhi > 0 ? (bhi + BN - 1) / BN : 0);
 
     float mul = 1.0f, undo = s.scale;                 // of ds, and of the sums
@@ -297,8 +304,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
         for (int i = 0; i < 16; ++i) dq[d][i] = 0.0f;
 
     const uint32_t plain_at = at_address(lds) + at_plain_lane<DP>(lane), trans_at = at_address(lds) + at_trans_lane<DP>(lane);
-    auto work = [&](int cur, int j0, auto masked) __attribute__((always_inline)) {
-        constexpr bool kMasked = decltype(masked)::value;
+    auto work = [&](int cur, int j0, bool whole) __attribute__((always_inline)) {
         const uint32_t ka = plain_at + cur * 2 * Tile::kBytes, va = ka + Tile::kBytes, kt = trans_at + cur * 2 * Tile::kBytes;
 #pragma unroll
         for (int t = 0; t < kSub; ++t) {
@@ -313,41 +319,34 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
             }
             const int first = j0 + t * 32 + 4 * half;
             const float away = BIAS ? float(place - first) : 0.0f;
-            u32x4 ds[2], seen[2];
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                bool vis[8];
-                float z[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int i = 8 * g + e;
-                    float slope = 1.0f, p;
-                    if (!CAP && !BIAS) {
-                        p = at_exp2(fmaf(x[i], s.c, -lse2));
-                    } else {
-                        float sc = ab_score<CAP>(s, x[i], slope);
-                        if (BIAS) sc = fmaf(-slope2, fabsf(away - float(at_reg_row(i))), sc);
-                        p = at_exp2(sc - lse2);
-                    }
-                    z[e] = p * (y[i] - delta);
-                    if (CAP) z[e] *= slope;
-                    if (Num::kHalf) z[e] *= mul;
-                    if (kMasked) {
-                        vis[e] = uint32_t(first + at_reg_row(i) - lo) < uint32_t(hi - lo);
-                        z[e] = vis[e] ? z[e] : 0.0f;
-                    }
+            for (int i = 0; i < 16; ++i) {
+                float slope = 1.0f, p;
+                if (!CAP && !BIAS) {
+                    p = at_exp2(fmaf(x[i], s.c, -lse2));
+                } else {
+                    float sc = ab_score<CAP>(s, x[i], slope);
+                    if (BIAS) sc = fmaf(-slope2, fabsf(away - float(at_reg_row(i))), sc);
+                    p = at_exp2(sc - lse2);
                 }
-#pragma unroll
-                for (int w = 0; w < 4; ++w) ds[g][w] = Num::pack(z[2 * w], z[2 * w + 1]);
-                if (kMasked) seen[g] = at_seen(vis, lane);
+                x[i] = p * (y[i] - delta);
+                if (CAP) x[i] *= slope;
+                if (Num::kHalf) x[i] *= mul;
             }
+            if (!whole) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = uint32_t(first + at_reg_row(i) - lo) < uint32_t(hi - lo) ? x[i] : 0.0f;
+            }
+            u32x4 ds[2];
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) ds[g][w] = Num::pack(x[8 * g + 2 * w], x[8 * g + 2 * w + 1]);
 #pragma unroll
             for (int g = 0; g < 2; ++g)
 #pragma unroll
                 for (int d = 0; d < kDt; ++d) {
-                    u32x4 f = at_transposed<DP>(kt, t * 32 + g * 16, d * 32);
-                    if (kMasked) f &= seen[g];
-                    dq[d] = Num::mfma(f, ds[g], dq[d]);
+                    dq[d] = Num::mfma(at_transposed<DP>(kt, t * 32 + g * 16, d * 32), ds[g], dq[d]);
                     if (d == kDt - 1) __builtin_amdgcn_sched_barrier(0);
                 }
         }
@@ -355,14 +354,18 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
     if (t0 < t1) fetch(t0);
     for (int t = t0, cur = 0; t < t1; ++t, cur ^= 1) {
         char *lk = lds + cur * 2 * Tile::kBytes, *lv = lk + Tile::kBytes;
+        const int j0 = t * BN;
+        if (j0 < all_lo || j0 + BN > all_hi) {
+            const uint64_t some = at_seen<NW>(seen, wave, lane, j0, lo, hi);
+            tk.keep(some);
+            tv.keep(some);
+        }
         tk.store(lk);
         tv.store(lv);
         __syncthreads();
         if (t + 1 < t1) fetch(t + 1);
-        const int j0 = t * BN;
         if (j0 + BN <= wlo || j0 >= whi) continue;
-        if (j0 >= flo && j0 + BN <= fhi) work(cur, j0, std::false_type());
-        else work(cur, j0, std::true_type());
+        work(cur, j0, j0 >= flo && j0 + BN <= fhi);
     }
     if (r_own >= s.R) return;
     char *p = a.dq.p + int64_t(b) * a.dq.batch + int64_t(row.token) * a.dq.token + int64_t(hq) * a.dq.head;

@@ -103,7 +103,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_fwd(const AtFwd a)
     typedef AtTile<NW * 64, BN, DP> Tile;
     constexpr int kKs = DP / 16, kDt = DP / 32, kSub = BN / 32;
     __shared__ __attribute__((aligned(128))) char lds[4 * Tile::kBytes];      // two tiles of k, two of v
-    __shared__ int range[2][NW];
+    __shared__ int range[4][NW];
+    __shared__ uint64_t seen[NW];
     const AtShape &s = a.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), half = lane >> 5;
     const uint32_t head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads;     // the heads first: a head's workgroups stay on one XCD where they are a multiple of 8
@@ -120,6 +121,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_fwd(const AtFwd a)
     if (lane == 0) {
         range[0][wave] = wlo;
         range[1][wave] = whi;
+        range[2][wave] = flo;
+        range[3][wave] = fhi;
     }
     u32x4 qf[kKs];
     {
@@ -130,12 +133,16 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_fwd(const AtFwd a)
     const float slope2 = BIAS ? s.slopes[hq] * kLog2e : 0.0f;
     const int place = BIAS ? at_place(s, b, row.token) : 0;
     __syncthreads();
-    int blo = 0x7FFFFFFF, bhi = 0;
+    int blo = 0x7FFFFFFF, bhi = 0, all_lo = 0, all_hi = 0x7FFFFFFF;      // the same of the workgroup's rows
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
         blo = range[0][w] < blo ? range[0][w] : blo;
         bhi = range[1][w] > bhi ? range[1][w] : bhi;
+        all_lo = range[2][w] > all_lo ? range[2][w] : all_lo;
+        all_hi = range[3][w] < all_hi ? range[3][w] : all_hi;
     }
+    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+    all_hi = __builtin_amdgcn_readfirstlane(all_hi);
     int t0 = bhi > 0 ? blo / BN : 0, t1 = bhi > 0 ? (bhi + BN - 1) / BN : 0;
     if (a.splits > 1) {
         const int per = (t1 - t0 + int(a.splits) - 1) / int(a.splits);
@@ -161,8 +168,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_fwd(const AtFwd a)
     float m = kAtLow, l = 0.0f;
 
     const uint32_t plain_at = at_address(lds) + at_plain_lane<DP>(lane), trans_at = at_address(lds) + at_trans_lane<DP>(lane);
-    auto work = [&](int cur, int j0, auto masked) __attribute__((always_inline)) {
-        constexpr bool kMasked = decltype(masked)::value;
+    auto work = [&](int cur, int j0, bool whole) __attribute__((always_inline)) {
         const uint32_t ka = plain_at + cur * 2 * Tile::kBytes, va = trans_at + cur * 2 * Tile::kBytes + Tile::kBytes;
         at_acc x[kSub];
 #pragma unroll
@@ -176,7 +182,6 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_fwd(const AtFwd a)
             }
         }
         const int first = j0 + 4 * half;           // the key of register 0
-        u32x4 seen[2 * kSub];
         if (CAP || BIAS) {
             const float away = float(place - first);
 #pragma unroll
@@ -188,20 +193,11 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_fwd(const AtFwd a)
                     if (BIAS) x[t][i] = fmaf(-slope2, fabsf(away - float(t * 32 + at_reg_row(i))), x[t][i]);
                 }
         }
-        if (kMasked) {
+        if (!whole) {
 #pragma unroll
             for (int t = 0; t < kSub; ++t)
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    bool vis[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int j = first + t * 32 + at_reg_row(8 * g + e);
-                        vis[e] = uint32_t(j - lo) < uint32_t(hi - lo);
-                        x[t][8 * g + e] = vis[e] ? x[t][8 * g + e] : -__builtin_inff();
-                    }
-                    seen[2 * t + g] = at_seen(vis, lane);
-                }
+                for (int i = 0; i < 16; ++i) x[t][i] = uint32_t(first + t * 32 + at_reg_row(i) - lo) < uint32_t(hi - lo) ? x[t][i] : -__builtin_inff();
         }
         float top = x[0][0];
 #pragma unroll
@@ -240,9 +236,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_fwd(const AtFwd a)
         for (int g = 0; g < 2 * kSub; ++g)
 #pragma unroll
             for (int d = 0; d < kDt; ++d) {
-                u32x4 f = at_transposed<DP>(va, g * 16, d * 32);
-                if (kMasked) f &= seen[g];
-                o[d] = Num::mfma(f, p[g], o[d]);
+                o[d] = Num::mfma(at_transposed<DP>(va, g * 16, d * 32), p[g], o[d]);
                 if (d == kDt - 1) __builtin_amdgcn_sched_barrier(0);
             }
     };
@@ -250,14 +244,18 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_fwd(const AtFwd a)
     if (t0 < t1) fetch(t0);
     for (int t = t0, cur = 0; t < t1; ++t, cur ^= 1) {
         char *lk = lds + cur * 2 * Tile::kBytes, *lv = lk + Tile::kBytes;
+        const int j0 = t * BN;
+        if (j0 < all_lo || j0 + BN > all_hi) {
+            const uint64_t some = at_seen<NW>(seen, wave, lane, j0, lo, hi);
+            tk.keep(some);
+            tv.keep(some);
+        }
         tk.store(lk);
         tv.store(lv);
         __syncthreads();                            // the other pair of tiles is behind every wave then
         if (t + 1 < t1) fetch(t + 1);
-        const int j0 = t * BN;
         if (j0 + BN <= wlo || j0 >= whi) continue;
-        if (j0 >= flo && j0 + BN <= fhi) work(cur, j0, std::false_type());
-        else work(cur, j0, std::true_type());
+        work(cur, j0, j0 >= flo && j0 + BN <= fhi);
     }
 
     l = at_pair_sum(l);
