@@ -109,7 +109,8 @@ def _load_fast():
         spec = importlib.util.spec_from_file_location("paper_2111_11124_amd._marshal", _FAST_PATH)
         fast = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(fast)
-        fast.setup(torch.float16, torch.float32, torch.bfloat16, Conv2d, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+        fast.setup(torch.float16, torch.float32, torch.bfloat16, Conv2d, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch.int8, torch.int32,
+                   QkvHeads, Attention)
         return fast
     except (ImportError, AttributeError):
         return _General()
@@ -532,6 +533,11 @@ def _qkv(heads, dtype, gamma_q, gamma_k, freq, pos, alpha, beta, rstd, every=Tru
 
 def mesa_qkv_norm_rope_fwd_q(x, heads: QkvHeads, gamma_q, gamma_k, freq, pos, alpha, beta, lam, y, rstd, q, ws, mode=ROUND_STOCHASTIC, seed=0, offset=0):
     """x (T, (Hq+Hk+Hv)*D or more) may be a slice of wider rows; y (T, Hq+Hk, D), q (T, Hq+Hk+Hv, D)"""
+    st = _fast.qkv_norm_rope_fwd_q(x, heads, gamma_q, gamma_k, freq, pos, alpha, beta, lam, y, rstd, q, ws, mode, seed, offset) if _lib is not None else None
+    if st is not None:
+        if st:
+            _check(st, "mesa_qkv_norm_rope_fwd_q")
+        return
     n = heads.Hq + heads.Hk
     h = n + heads.Hv
     dt = _dt(x)
@@ -544,6 +550,11 @@ def mesa_qkv_norm_rope_fwd_q(x, heads: QkvHeads, gamma_q, gamma_k, freq, pos, al
 
 
 def mesa_qkv_norm_rope_recompute_q(q, heads: QkvHeads, gamma_q, gamma_k, freq, pos, alpha, beta, rstd, y):
+    st = _fast.qkv_norm_rope_recompute_q(q, heads, gamma_q, gamma_k, freq, pos, alpha, beta, rstd, y) if _lib is not None else None
+    if st is not None:
+        if st:
+            _check(st, "mesa_qkv_norm_rope_recompute_q")
+        return
     n = heads.Hq + heads.Hk
     dt = _dt(y)
     gq, gk, fr, ps, al, be, rs = _qkv(heads, y.dtype, gamma_q, gamma_k, freq, pos, alpha, beta, rstd)
@@ -553,10 +564,15 @@ def mesa_qkv_norm_rope_recompute_q(q, heads: QkvHeads, gamma_q, gamma_k, freq, p
 
 def mesa_qkv_norm_rope_bwd_q(q, heads: QkvHeads, gamma_q, gamma_k, freq, pos, alpha, beta, rstd, dy, dx, dgamma_q, dgamma_k, ws):
     """dy (T, Hq+Hk, D); dx (T, Hq+Hk, D) or (T, (Hq+Hk)*D or more), a slice of wider rows: what lies beyond the Hq+Hk heads stays as it is"""
-    n = heads.Hq + heads.Hk
-    dt = _dt(dy)
     if dx.dim() == 3 and dx.is_contiguous():
         dx = dx.view(dx.shape[0], -1)
+    st = _fast.qkv_norm_rope_bwd_q(q, heads, gamma_q, gamma_k, freq, pos, alpha, beta, rstd, dy, dx, dgamma_q, dgamma_k, ws) if _lib is not None else None
+    if st is not None:
+        if st:
+            _check(st, "mesa_qkv_norm_rope_bwd_q")
+        return
+    n = heads.Hq + heads.Hk
+    dt = _dt(dy)
     pdx, row = _rows(dx, dy.dtype, heads.T, n * heads.D, "dx")
     gq, gk, fr, ps, al, be, rs = _qkv(heads, dy.dtype, gamma_q, gamma_k, freq, pos, alpha, beta, rstd)
     p, size = _ws_args(ws)
@@ -567,6 +583,11 @@ def mesa_qkv_norm_rope_bwd_q(q, heads: QkvHeads, gamma_q, gamma_k, freq, pos, al
 
 def mesa_attention_bounds(lo, hi, Nk, causal, window=0, kv_len=None, q_start=None, prefix=None, doc=None):
     """lo, hi (B, Nq) int32; kv_len, q_start, prefix [B], doc (B, Nk) int32"""
+    st = _fast.attention_bounds(lo, hi, Nk, causal, window, kv_len, q_start, prefix, doc) if _lib is not None else None
+    if st is not None:
+        if st:
+            _check(st, "mesa_attention_bounds")
+        return
     if lo.dim() != 2 or lo.shape != hi.shape:
         raise ValueError("lo and hi are (B, Nq)")
     B, Nq = lo.shape
@@ -598,6 +619,11 @@ def _mask(a, lo, hi, slopes, q_start):
 
 def mesa_attention_fwd(a: Attention, q, k, v, o, lse, ws=None, lo=None, hi=None, slopes=None, q_start=None):
     """q, o (B, Nq, Hq, D), k, v (B, Nk, Hk, D), any strides that are multiples of 8 with a head's elements side by side; lse (B, Hq, Nq)"""
+    st = _fast.attention_fwd(a, q, k, v, o, lse, ws, lo, hi, slopes, q_start) if _lib is not None else None
+    if st is not None:
+        if st:
+            _check(st, "mesa_attention_fwd")
+        return
     dt, d = _dt(q), q.dtype
     rows, keys = (a.B, a.Nq, a.Hq, a.D), (a.B, a.Nk, a.Hk, a.D)
     p, size = _ws_args(ws)
@@ -607,6 +633,11 @@ def mesa_attention_fwd(a: Attention, q, k, v, o, lse, ws=None, lo=None, hi=None,
 
 def mesa_attention_bwd_q(a: Attention, q, k, v, o, lse, do, dq, dk, dv, ws, lo=None, hi=None, slopes=None, q_start=None):
     """q, k, v: tensors of the storage type, or (codes, alpha, beta) each; shapes and strides as for the forward"""
+    st = _fast.attention_bwd_q(a, q, k, v, o, lse, do, dq, dk, dv, ws, lo, hi, slopes, q_start) if _lib is not None else None
+    if st is not None:
+        if st:
+            _check(st, "mesa_attention_bwd_q")
+        return
     dt, d = _dt(do), do.dtype
     rows, keys = (a.B, a.Nq, a.Hq, a.D), (a.B, a.Nk, a.Hk, a.D)
     p, size = _ws_args(ws)

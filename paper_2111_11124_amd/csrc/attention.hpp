@@ -143,6 +143,8 @@ template <int NT, int ROWS, int DP> struct AtTile {
     }
 };
 
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Wint-to-pointer-cast"      // the host pass counts pointers in 64 bits
 // LDS by its 32-bit address: a lane's place in a tile is one register for plain reads and one for transposing ones; which
 // piece a read takes is an exclusive-or with a constant (tiles start at multiples of 128 bytes), the row an immediate offset.
 __device__ __forceinline__ uint32_t at_address(const char *lds) { return uint32_t(uintptr_t((__attribute__((address_space(3))) const char *)lds)); }
@@ -168,6 +170,8 @@ template <int DP> __device__ __forceinline__ u32x4 at_transposed(uint32_t at, in
     const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)(p + 8 * DP * 2)));
     return u32x4{a[0], a[1], b[0], b[1]};
 }
+
+#pragma clang diagnostic pop
 
 // B operand straight from memory: elements 16*ks + 8*(lane/32) ..+7 of the lane's row, zeros past D
 __device__ __forceinline__ u32x4 at_column(const char *row, int ks, int lane, int D)

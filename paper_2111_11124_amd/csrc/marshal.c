@@ -21,7 +21,10 @@
 
 static PyObject *n_is_cuda, *n_is_contiguous, *n_data_ptr, *n_dtype, *n_numel, *n_element_size;
 static PyObject *t_f16, *t_f32, *t_bf16;          /* torch.float16, torch.float32, torch.bfloat16 */
+static PyObject *t_i8, *t_i32;                    /* torch.int8, torch.int32 */
 static PyObject *conv_type;                       /* the binding's Conv2d structure */
+static PyObject *heads_type, *attention_type;     /* its QkvHeads and Attention */
+static PyObject *n_get_device, *n_shape, *n_stride;
 static PyObject *get_device, *get_raw_stream;     /* torch._C._cuda_getDevice, _cuda_getCurrentRawStream */
 
 struct call {
@@ -582,13 +585,260 @@ ENTRY(attn_qk_bwd_q, 14)
     RUN(c, mesa_attn_qk_bwd_q(qq, kq, B, H, N, Dh, alpha_q, beta_q, alpha_k, beta_k, dS, scale, dQ, dK, dt, stream));
 }
 
-/* setup(float16, float32, bfloat16, Conv2d, get_device, get_raw_stream) */
+/* ---- a language model's attention block: tensors with a type, a size and the current device to check, and strided ones ---- */
+static void take_struct(struct call *c, int i, PyObject *type, void *out, size_t size)
+{
+    memset(out, 0, size);
+    Py_buffer b;
+    if (!c->ok) return;
+    if ((PyObject *)Py_TYPE(c->args[i]) != type || PyObject_GetBuffer(c->args[i], &b, PyBUF_SIMPLE) != 0) { c->ok = 0; return; }
+    if (b.len == (Py_ssize_t)size) memcpy(out, b.buf, size);
+    else c->ok = 0;
+    PyBuffer_Release(&b);
+}
+
+static long long int_result(struct call *c, PyObject *p)
+{
+    if (!p || !PyLong_Check(p)) { Py_XDECREF(p); c->ok = 0; return 0; }
+    const long long v = PyLong_AsLongLong(p);
+    Py_DECREF(p);
+    return v;
+}
+
+static long long current_device(struct call *c) { return c->ok ? int_result(c, PyObject_CallNoArgs(get_device)) : -1; }
+
+/* a tensor of that type on the current device: its address */
+static void *typed(struct call *c, PyObject *t, PyObject *type, long long device)
+{
+    if (!c->ok) return NULL;
+    PyObject *d = PyObject_GetAttr(t, n_dtype);
+    Py_XDECREF(d);
+    if (!d || d != type || int_result(c, PyObject_CallMethodNoArgs(t, n_get_device)) != device || !c->ok) { c->ok = 0; return NULL; }
+    return (void *)(uintptr_t)int_result(c, PyObject_CallMethodNoArgs(t, n_data_ptr));
+}
+
+static void *flat_of(struct call *c, PyObject *t, PyObject *type, int64_t count, long long device)
+{
+    if (!c->ok || t == Py_None) return NULL;
+    void *p = typed(c, t, type, device);
+    if (c->ok && truth(PyObject_CallMethodNoArgs(t, n_is_contiguous)) != 1) c->ok = 0;
+    if (c->ok && (int64_t)take_size(c, t, n_numel) < count) c->ok = 0;
+    return p;
+}
+static void *take_flat(struct call *c, int i, PyObject *type, int64_t count, long long device) { return c->ok ? flat_of(c, c->args[i], type, count, device) : NULL; }
+
+/* sizes or strides, n of them */
+static void take_sizes(struct call *c, PyObject *v, int n, int64_t *out)
+{
+    if (!v || !PyTuple_Check(v) || PyTuple_GET_SIZE(v) != n) c->ok = 0;
+    for (int k = 0; c->ok && k < n; ++k) {
+        out[k] = PyLong_AsLongLong(PyTuple_GET_ITEM(v, k));
+        if (out[k] == -1 && PyErr_Occurred()) c->ok = 0;
+    }
+    Py_XDECREF(v);
+}
+
+/* (rows, at least width) with elements side by side */
+static void *take_rows(struct call *c, int i, PyObject *type, int64_t rows, int64_t width, long long device, int64_t *row)
+{
+    int64_t size[2], step[2];
+    *row = 0;
+    void *p = c->ok ? typed(c, c->args[i], type, device) : NULL;
+    if (!c->ok) return NULL;
+    take_sizes(c, PyObject_GetAttr(c->args[i], n_shape), 2, size);
+    take_sizes(c, c->ok ? PyObject_CallMethodNoArgs(c->args[i], n_stride) : NULL, 2, step);
+    if (!c->ok || size[0] != rows || size[1] < width || (size[1] > 1 && step[1] != 1)) { c->ok = 0; return NULL; }
+    *row = rows > 1 ? step[0] : size[1] < 8 ? 8 : (size[1] + 7) / 8 * 8;
+    return p;
+}
+
+/* (B, tokens, heads, D) with a head's elements side by side */
+static mesa_attention_in view_of(struct call *c, PyObject *t, PyObject *type, const int64_t want[4], long long device)
+{
+    mesa_attention_in x = {NULL, 0, 0, 0, NULL, NULL};
+    int64_t size[4], step[4];
+    x.data = typed(c, t, type, device);
+    if (!c->ok) return x;
+    take_sizes(c, PyObject_GetAttr(t, n_shape), 4, size);
+    take_sizes(c, c->ok ? PyObject_CallMethodNoArgs(t, n_stride) : NULL, 4, step);
+    for (int k = 0; c->ok && k < 4; ++k)
+        if (size[k] != want[k]) c->ok = 0;
+    if (!c->ok || (size[3] > 1 && step[3] != 1)) { c->ok = 0; return x; }
+    x.batch = size[0] > 1 ? step[0] : 0;
+    x.token = size[1] > 1 ? step[1] : 0;
+    x.head = size[2] > 1 ? step[2] : 0;
+    return x;
+}
+/* a tensor, or (codes, alpha, beta) */
+static mesa_attention_in take_operand(struct call *c, int i, PyObject *type, const int64_t want[4], long long device)
+{
+    mesa_attention_in x = {NULL, 0, 0, 0, NULL, NULL};
+    if (!c->ok) return x;
+    PyObject *t = c->args[i];
+    if (!PyTuple_CheckExact(t)) return view_of(c, t, type, want, device);
+    if (PyTuple_GET_SIZE(t) != 3 || PyTuple_GET_ITEM(t, 1) == Py_None || PyTuple_GET_ITEM(t, 2) == Py_None) { c->ok = 0; return x; }
+    x = view_of(c, PyTuple_GET_ITEM(t, 0), t_i8, want, device);
+    x.alpha = flat_of(c, PyTuple_GET_ITEM(t, 1), t_f32, want[2], device);
+    x.beta = flat_of(c, PyTuple_GET_ITEM(t, 2), t_f32, want[2], device);
+    return x;
+}
+static mesa_attention_out take_result(struct call *c, int i, PyObject *type, const int64_t want[4], long long device)
+{
+    mesa_attention_out o = {NULL, 0, 0, 0};
+    if (!c->ok) return o;
+    const mesa_attention_in x = view_of(c, c->args[i], type, want, device);
+    o.data = (void *)x.data;
+    o.batch = x.batch;
+    o.token = x.token;
+    o.head = x.head;
+    return o;
+}
+static mesa_attention_mask take_mask(struct call *c, int i, const mesa_attention *a, long long device)   /* lo, hi, slopes, q_start */
+{
+    mesa_attention_mask m;
+    m.lo = take_flat(c, i, t_i32, a->B * a->Nq, device);
+    m.hi = take_flat(c, i + 1, t_i32, a->B * a->Nq, device);
+    m.slopes = take_flat(c, i + 2, t_f32, a->Hq, device);
+    m.q_start = take_flat(c, i + 3, t_i32, a->B, device);
+    return m;
+}
+static PyObject *type_of(mesa_dtype dt) { return dt == MESA_F16 ? t_f16 : dt == MESA_BF16 ? t_bf16 : t_f32; }
+/* sizes that a product of a few of them stays in range for: what does not is left to the general path */
+static void small(struct call *c, const int64_t *v, int n)
+{
+    for (int k = 0; k < n; ++k)
+        if (v[k] < 0 || v[k] >= ((int64_t)1 << 31)) c->ok = 0;
+}
+
+ENTRY(qkv_norm_rope_fwd_q, 16)
+{
+    struct call c = begin(args, nargs, 16);
+    mesa_qkv_heads h;
+    take_struct(&c, 1, heads_type, &h, sizeof h);
+    small(&c, &h.T, 6);
+    const long long dev = current_device(&c);
+    const mesa_dtype dt = take_dtype(&c, 0);
+    PyObject *type = type_of(dt);
+    const int64_t n = h.Hq + h.Hk, every = n + h.Hv;
+    int64_t row;
+    void *x = take_rows(&c, 0, type, h.T, every * h.D, dev, &row);
+    void *gq = take_flat(&c, 2, type, h.D, dev), *gk = take_flat(&c, 3, type, h.D, dev), *freq = take_flat(&c, 4, t_f32, h.rot / 2, dev);
+    void *pos = take_flat(&c, 5, t_i32, h.axes * h.T, dev), *alpha = take_flat(&c, 6, t_f32, every, dev), *beta = take_flat(&c, 7, t_f32, every, dev);
+    const float lam = take_float(&c, 8);
+    void *y = take_flat(&c, 9, type, h.T * n * h.D, dev), *rstd = take_flat(&c, 10, t_f32, h.T * n, dev), *q = take_flat(&c, 11, t_i8, h.T * every * h.D, dev);
+    size_t ws_bytes;
+    void *ws = take_ws(&c, 12, &ws_bytes);
+    const int mode = (int)take_int(&c, 13);
+    const uint64_t seed = take_int(&c, 14), offset = take_int(&c, 15);
+    RUN(c, mesa_qkv_norm_rope_fwd_q(x, row, h, gq, gk, freq, pos, alpha, beta, lam, y, rstd, q, mode, seed, offset, ws, ws_bytes, dt, stream));
+}
+
+ENTRY(qkv_norm_rope_recompute_q, 10)
+{
+    struct call c = begin(args, nargs, 10);
+    mesa_qkv_heads h;
+    take_struct(&c, 1, heads_type, &h, sizeof h);
+    small(&c, &h.T, 6);
+    const long long dev = current_device(&c);
+    const mesa_dtype dt = take_dtype(&c, 9);
+    PyObject *type = type_of(dt);
+    const int64_t n = h.Hq + h.Hk, every = n + h.Hv;
+    void *q = take_flat(&c, 0, t_i8, h.T * every * h.D, dev);
+    void *gq = take_flat(&c, 2, type, h.D, dev), *gk = take_flat(&c, 3, type, h.D, dev), *freq = take_flat(&c, 4, t_f32, h.rot / 2, dev);
+    void *pos = take_flat(&c, 5, t_i32, h.axes * h.T, dev), *alpha = take_flat(&c, 6, t_f32, every, dev), *beta = take_flat(&c, 7, t_f32, every, dev);
+    void *rstd = take_flat(&c, 8, t_f32, h.T * n, dev), *y = take_flat(&c, 9, type, h.T * n * h.D, dev);
+    RUN(c, mesa_qkv_norm_rope_recompute_q(q, h, gq, gk, freq, pos, alpha, beta, rstd, y, dt, stream));
+}
+
+ENTRY(qkv_norm_rope_bwd_q, 14)
+{
+    struct call c = begin(args, nargs, 14);
+    mesa_qkv_heads h;
+    take_struct(&c, 1, heads_type, &h, sizeof h);
+    small(&c, &h.T, 6);
+    const long long dev = current_device(&c);
+    const mesa_dtype dt = take_dtype(&c, 9);
+    PyObject *type = type_of(dt);
+    const int64_t n = h.Hq + h.Hk, every = n + h.Hv;
+    void *q = take_flat(&c, 0, t_i8, h.T * every * h.D, dev);
+    void *gq = take_flat(&c, 2, type, h.D, dev), *gk = take_flat(&c, 3, type, h.D, dev), *freq = take_flat(&c, 4, t_f32, h.rot / 2, dev);
+    void *pos = take_flat(&c, 5, t_i32, h.axes * h.T, dev), *alpha = take_flat(&c, 6, t_f32, every, dev), *beta = take_flat(&c, 7, t_f32, every, dev);
+    void *rstd = take_flat(&c, 8, t_f32, h.T * n, dev), *dy = take_flat(&c, 9, type, h.T * n * h.D, dev);
+    int64_t row;
+    void *dx = take_rows(&c, 10, type, h.T, n * h.D, dev, &row);
+    void *dgq = take_flat(&c, 11, t_f32, h.D, dev), *dgk = take_flat(&c, 12, t_f32, h.D, dev);
+    size_t ws_bytes;
+    void *ws = take_ws(&c, 13, &ws_bytes);
+    RUN(c, mesa_qkv_norm_rope_bwd_q(q, h, gq, gk, freq, pos, alpha, beta, rstd, dy, dx, row, dgq, dgk, ws, ws_bytes, dt, stream));
+}
+
+ENTRY(attention_bounds, 9)
+{
+    struct call c = begin(args, nargs, 9);
+    const long long dev = current_device(&c);
+    int64_t size[2] = {0, 0};
+    if (c.ok) take_sizes(&c, PyObject_GetAttr(c.args[0], n_shape), 2, size);
+    const int64_t Nk = (int64_t)take_int(&c, 2);
+    const int64_t all[3] = {size[0], size[1], Nk};
+    small(&c, all, 3);
+    int64_t other[2];
+    if (c.ok) take_sizes(&c, PyObject_GetAttr(c.args[1], n_shape), 2, other);
+    if (c.ok && (other[0] != size[0] || other[1] != size[1])) c.ok = 0;
+    void *lo = take_flat(&c, 0, t_i32, size[0] * size[1], dev), *hi = take_flat(&c, 1, t_i32, size[0] * size[1], dev);
+    const int causal = take_bool(&c, 3);
+    const int64_t window = (int64_t)take_int(&c, 4);
+    void *kv_len = take_flat(&c, 5, t_i32, size[0], dev), *q_start = take_flat(&c, 6, t_i32, size[0], dev), *prefix = take_flat(&c, 7, t_i32, size[0], dev);
+    void *doc = take_flat(&c, 8, t_i32, size[0] * Nk, dev);
+    RUN(c, mesa_attention_bounds(lo, hi, size[0], size[1], Nk, causal, window, kv_len, q_start, prefix, doc, stream));
+}
+
+ENTRY(attention_fwd, 11)
+{
+    struct call c = begin(args, nargs, 11);
+    mesa_attention a;
+    take_struct(&c, 0, attention_type, &a, sizeof a);
+    small(&c, &a.B, 6);
+    const long long dev = current_device(&c);
+    const mesa_dtype dt = take_dtype(&c, 1);
+    PyObject *type = type_of(dt);
+    const int64_t rows[4] = {a.B, a.Nq, a.Hq, a.D}, keys[4] = {a.B, a.Nk, a.Hk, a.D};
+    const mesa_attention_in q = take_operand(&c, 1, type, rows, dev), k = take_operand(&c, 2, type, keys, dev), v = take_operand(&c, 3, type, keys, dev);
+    const mesa_attention_out o = take_result(&c, 4, type, rows, dev);
+    void *lse = take_flat(&c, 5, t_f32, a.B * a.Hq * a.Nq, dev);
+    size_t ws_bytes;
+    void *ws = take_ws(&c, 6, &ws_bytes);
+    const mesa_attention_mask m = take_mask(&c, 7, &a, dev);
+    RUN(c, mesa_attention_fwd(a, q, k, v, o, lse, m, ws, ws_bytes, dt, stream));
+}
+
+ENTRY(attention_bwd_q, 15)
+{
+    struct call c = begin(args, nargs, 15);
+    mesa_attention a;
+    take_struct(&c, 0, attention_type, &a, sizeof a);
+    small(&c, &a.B, 6);
+    const long long dev = current_device(&c);
+    const mesa_dtype dt = take_dtype(&c, 6);
+    PyObject *type = type_of(dt);
+    const int64_t rows[4] = {a.B, a.Nq, a.Hq, a.D}, keys[4] = {a.B, a.Nk, a.Hk, a.D};
+    const mesa_attention_in q = take_operand(&c, 1, type, rows, dev), k = take_operand(&c, 2, type, keys, dev), v = take_operand(&c, 3, type, keys, dev);
+    const mesa_attention_in o = take_operand(&c, 4, type, rows, dev);
+    void *lse = take_flat(&c, 5, t_f32, a.B * a.Hq * a.Nq, dev);
+    const mesa_attention_in dO = take_operand(&c, 6, type, rows, dev);
+    const mesa_attention_out dq = take_result(&c, 7, type, rows, dev), dk = take_result(&c, 8, type, keys, dev), dv = take_result(&c, 9, type, keys, dev);
+    size_t ws_bytes;
+    void *ws = take_ws(&c, 10, &ws_bytes);
+    const mesa_attention_mask m = take_mask(&c, 11, &a, dev);
+    RUN(c, mesa_attention_bwd_q(a, q, k, v, o, lse, dO, dq, dk, dv, m, ws, ws_bytes, dt, stream));
+}
+
+/* setup(float16, float32, bfloat16, Conv2d, get_device, get_raw_stream, int8, int32, QkvHeads, Attention) */
 static PyObject *py_setup(PyObject *self, PyObject *args)
 {
-    PyObject *o[6];
-    if (!PyArg_ParseTuple(args, "OOOOOO", &o[0], &o[1], &o[2], &o[3], &o[4], &o[5])) return NULL;
-    PyObject **slot[6] = {&t_f16, &t_f32, &t_bf16, &conv_type, &get_device, &get_raw_stream};
-    for (int i = 0; i < 6; ++i) {
+    PyObject *o[10];
+    if (!PyArg_ParseTuple(args, "OOOOOOOOOO", &o[0], &o[1], &o[2], &o[3], &o[4], &o[5], &o[6], &o[7], &o[8], &o[9])) return NULL;
+    PyObject **slot[10] = {&t_f16, &t_f32, &t_bf16, &conv_type, &get_device, &get_raw_stream, &t_i8, &t_i32, &heads_type, &attention_type};
+    for (int i = 0; i < 10; ++i) {
         Py_INCREF(o[i]);
         Py_XSETREF(*slot[i], o[i]);
     }
@@ -622,6 +872,12 @@ static PyMethodDef methods[] = {
     METHOD(conv2d_dw_q),
     METHOD(attn_av_bwd_q),
     METHOD(attn_qk_bwd_q),
+    METHOD(qkv_norm_rope_fwd_q),
+    METHOD(qkv_norm_rope_recompute_q),
+    METHOD(qkv_norm_rope_bwd_q),
+    METHOD(attention_bounds),
+    METHOD(attention_fwd),
+    METHOD(attention_bwd_q),
     {NULL, NULL, 0, NULL},
 };
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};
@@ -631,6 +887,7 @@ PyMODINIT_FUNC PyInit__marshal(void)
     struct { PyObject **slot; const char *name; } names[] = {
         {&n_is_cuda, "is_cuda"}, {&n_is_contiguous, "is_contiguous"}, {&n_data_ptr, "data_ptr"},
         {&n_dtype, "dtype"}, {&n_numel, "numel"}, {&n_element_size, "element_size"},
+        {&n_get_device, "get_device"}, {&n_shape, "shape"}, {&n_stride, "stride"},
     };
     for (size_t i = 0; i < sizeof names / sizeof names[0]; ++i)
         if (!(*names[i].slot = PyUnicode_InternFromString(names[i].name))) return NULL;

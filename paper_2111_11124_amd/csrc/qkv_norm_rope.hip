@@ -22,6 +22,7 @@ namespace mesa {
 constexpr int kQkvTile = 32;        // tokens of a tile at most (cosines and sines of 32 x 128 pairs: 32 KB)
 constexpr int kQkvGrid = 1024;      // workgroups at most: four per compute unit
 constexpr int kQkvMaxHeads = 512;
+constexpr int kQkvAlone = 16384;    // elements at most that one workgroup takes
 constexpr int kQkvU = 4;            // tokens in flight per wave
 
 struct QkvGeom {
@@ -46,9 +47,12 @@ static QkvGeom qkv_geom(const mesa_qkv_heads &h)
     while ((8u << g.lph_log2) < g.D) ++g.lph_log2;
     // few tokens: tiles of fewer, so that there are workgroups for every compute unit
     int64_t t = ceil_div(h.T, kQkvGrid);
+    // so few that one workgroup does them: it moves the estimates, or adds up the gains' gradients, itself -- a second, dependent launch
+    // costs as much as the first
+    if (h.T <= kQkvTile && h.T * int64_t(g.H) * h.D <= kQkvAlone) t = h.T;
     g.tile = uint32_t(t < 1 ? 1 : t > kQkvTile ? kQkvTile : t);
     const uint32_t slots = (g.H << g.lph_log2) / 64 + (((g.H << g.lph_log2) % 64) != 0);
-    g.phases_log2 = slots >= 4 ? 0 : slots >= 2 ? 1 : 2;
+    g.phases_log2 = slots >= 4 || g.tile < 2 ? 0 : slots >= 2 || g.tile < 4 ? 1 : 2;      // no more parts than tokens
     uint32_t e = 0;
     for (int a = 0; a < 4; ++a) {
         if (a < h.axes) e += uint32_t(h.section[a]);
@@ -128,7 +132,7 @@ __device__ __forceinline__ void qkv_hat(u32x2 c, float s, float b, float f[8])
 template <typename T, bool SR, bool AGAIN>
 __global__ __launch_bounds__(kThreads) void k_qkv_fwd(QkvGeom g, const void *__restrict__ x, int64_t x_row, const int8_t *__restrict__ qin, const void *__restrict__ gamma_q,
                                                       const void *__restrict__ gamma_k, const float *__restrict__ freq, const int32_t *__restrict__ pos,
-                                                      const float *__restrict__ alpha, const float *__restrict__ beta, void *__restrict__ y, float *__restrict__ rstd,
+                                                      float *alpha, float *beta, float lambda, void *__restrict__ y, float *__restrict__ rstd,
                                                       int8_t *__restrict__ q, uint64_t seed, uint64_t offset, float *__restrict__ part)
 {
     typedef typename Store<T>::raw_t Raw;
@@ -227,6 +231,11 @@ __global__ __launch_bounds__(kThreads) void k_qkv_fwd(QkvGeom g, const void *__r
     }
     if (!AGAIN) {
         __syncthreads();
+        if (gridDim.x == 1) {
+            for (uint32_t h = threadIdx.x; h < g.H; h += kThreads)
+                ema_update(order_val(lmn[h]), order_val(lmx[h]), alpha[h], beta[h], alpha, beta, h, lambda, 0);
+            return;
+        }
         for (uint32_t h = threadIdx.x; h < g.H; h += kThreads) {
             part[int64_t(blockIdx.x) * 2 * g.H + h] = order_val(lmn[h]);
             part[int64_t(blockIdx.x) * 2 * g.H + g.H + h] = order_val(lmx[h]);
@@ -239,7 +248,7 @@ template <typename T, bool NORM>
 __global__ __launch_bounds__(kThreads) void k_qkv_bwd(QkvGeom g, const int8_t *__restrict__ q, const void *__restrict__ gamma_q, const void *__restrict__ gamma_k,
                                                       const float *__restrict__ freq, const int32_t *__restrict__ pos, const float *__restrict__ alpha,
                                                       const float *__restrict__ beta, const float *__restrict__ rstd, const void *dy, void *dx, int64_t dx_row,
-                                                      float *__restrict__ part)
+                                                      float *__restrict__ part, float *__restrict__ dgamma_q, float *__restrict__ dgamma_k)
 {
     typedef typename Store<T>::raw_t Raw;
     extern __shared__ float2 smem[];
@@ -336,7 +345,8 @@ __global__ __launch_bounds__(kThreads) void k_qkv_bwd(QkvGeom g, const int8_t *_
         const uint32_t c = i >= g.D, d = i - c * g.D;
         float v = 0.0f;
         for (uint32_t w = 0; w < kThreads / 64; ++w) v += sum[((w * 2 + c) << (g.lph_log2 + 3)) + d];
-        part[int64_t(blockIdx.x) * 2 * g.D + i] = v;
+        if (gridDim.x > 1) part[int64_t(blockIdx.x) * 2 * g.D + i] = v;
+        else (c ? dgamma_k : dgamma_q)[d] = v;
     }
 }
 
@@ -421,11 +431,12 @@ extern "C" MESA_EXPORT mesa_status mesa_qkv_norm_rope_fwd_q(const void *x, int64
 #define MESA_QKV(T) \
     do { \
         auto *k = mode == MESA_ROUND_STOCHASTIC ? k_qkv_fwd<T, true, false> : k_qkv_fwd<T, false, false>; \
-        hipLaunchKernelGGL(k, dim3(grid), dim3(kThreads), lds, s, g, x, x_row, nullptr, gamma_q, gamma_k, freq, pos, alpha, beta, y, rstd, q, seed, offset, static_cast<float *>(ws)); \
+        hipLaunchKernelGGL(k, dim3(grid), dim3(kThreads), lds, s, g, x, x_row, nullptr, gamma_q, gamma_k, freq, pos, alpha, beta, lambda, y, rstd, q, seed, offset, static_cast<float *>(ws)); \
     } while (0)
     MESA_FOR_DTYPE(dt, MESA_QKV);
 #undef MESA_QKV
     if (const mesa_status st = launch_status()) return st;
+    if (grid == 1) return MESA_OK;
     launch_ema_finalize(static_cast<const float *>(ws), grid, g.H, alpha, beta, lambda, 0, 0, 0.0f, s);
     return launch_status();
 }
@@ -443,8 +454,8 @@ extern "C" MESA_EXPORT mesa_status mesa_qkv_norm_rope_recompute_q(const int8_t *
     const QkvGeom g = qkv_geom(h);
     const size_t lds = qkv_lds(g, false);
 #define MESA_QKV(T) \
-    hipLaunchKernelGGL((k_qkv_fwd<T, false, true>), dim3(qkv_grid(g)), dim3(kThreads), lds, static_cast<hipStream_t>(stream), g, nullptr, 0, q, gamma_q, gamma_k, freq, pos, alpha, \
-                       beta, y, const_cast<float *>(rstd), nullptr, 0, 0, nullptr)
+    hipLaunchKernelGGL((k_qkv_fwd<T, false, true>), dim3(qkv_grid(g)), dim3(kThreads), lds, static_cast<hipStream_t>(stream), g, nullptr, 0, q, gamma_q, gamma_k, freq, pos, \
+                       const_cast<float *>(alpha), const_cast<float *>(beta), 0.0f, y, const_cast<float *>(rstd), nullptr, 0, 0, nullptr)
     MESA_FOR_DTYPE(dt, MESA_QKV);
 #undef MESA_QKV
     return launch_status();
@@ -475,13 +486,13 @@ extern "C" MESA_EXPORT mesa_status mesa_qkv_norm_rope_bwd_q(const int8_t *q, mes
 #define MESA_QKV(T) \
     do { \
         auto *k = norm ? k_qkv_bwd<T, true> : k_qkv_bwd<T, false>; \
-        hipLaunchKernelGGL(k, dim3(grid), dim3(kThreads), lds, s, g, q, gamma_q, gamma_k, freq, pos, alpha, beta, rstd, dy, dx, dx_row, static_cast<float *>(ws)); \
+        hipLaunchKernelGGL(k, dim3(grid), dim3(kThreads), lds, s, g, q, gamma_q, gamma_k, freq, pos, alpha, beta, rstd, dy, dx, dx_row, static_cast<float *>(ws), dgamma_q, dgamma_k); \
     } while (0)
         MESA_FOR_DTYPE(dt, MESA_QKV);
 #undef MESA_QKV
         if (const mesa_status st = launch_status()) return st;
     }
-    if (norm) {   // no tokens: zeros
+    if (norm && (h.T == 0 || grid > 1)) {   // no tokens: zeros
         hipLaunchKernelGGL(k_qkv_gains, dim3(uint32_t(ceil_div(2 * h.D, kQkvCols))), dim3(1024), 0, s, static_cast<const float *>(ws), h.T > 0 ? grid : 0, g.D, dgamma_q, dgamma_k);
         return launch_status();
     }

@@ -125,6 +125,28 @@ __device__ __forceinline__ float vmax3(float a, float b, float c) { float r; asm
 __device__ __forceinline__ uint32_t pkmin(uint32_t a, uint32_t b) { uint32_t r; asm("v_pk_min_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b)); return r; }
 __device__ __forceinline__ uint32_t pkmax(uint32_t a, uint32_t b) { uint32_t r; asm("v_pk_max_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b)); return r; }
 
+// Eq. (6)-(7) for one group from its extrema: each product, difference and sum rounded on its own.
+// (alpha_old, beta_old: the running estimates as they were, read by the caller ahead of time)
+__device__ __forceinline__ void ema_update(float mn, float mx, float alpha_old, float beta_old, float *alpha, float *beta,
+                                           uint32_t g, float lambda, int first_call)
+{
+    mn = mn + 0.0f;  // -0.0 -> +0.0
+    mx = mx + 0.0f;
+    float range = mx - mn;
+    if (first_call) {
+        alpha[g] = range;
+        beta[g] = mn;
+    } else {
+        float a = lambda * alpha_old;
+        float b = 1.0f - lambda;
+        float c = b * range;
+        alpha[g] = a + c;
+        float e = lambda * beta_old;
+        float f = b * mn;
+        beta[g] = e + f;
+    }
+}
+
 // Host side: combine the per-workgroup extrema part[nwg][2 * groups] (minima, then maxima) and move the running
 // estimates, Eq. (6)-(7); defined with the kernel in stream_kernels.hip.  variant: 0 plain, 1 symmetric range,
 // 2 fixed offset (beta_fixed).

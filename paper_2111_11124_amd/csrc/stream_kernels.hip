@@ -504,28 +504,6 @@ __global__ __launch_bounds__(kThreads) void k_minmax_partial_few(const void *__r
     store_tables(lmn, lmx, gg.groups, 1u, part);
 }
 
-// Eq. (6)-(7) for one group from its extrema: each product, difference and sum rounded on its own.
-// (alpha_old, beta_old: the running estimates as they were, read by the caller ahead of time)
-__device__ __forceinline__ void ema_update(float mn, float mx, float alpha_old, float beta_old, float *alpha, float *beta,
-                                           uint32_t g, float lambda, int first_call)
-{
-    mn = mn + 0.0f;  // -0.0 -> +0.0
-    mx = mx + 0.0f;
-    float range = mx - mn;
-    if (first_call) {
-        alpha[g] = range;
-        beta[g] = mn;
-    } else {
-        float a = lambda * alpha_old;
-        float b = 1.0f - lambda;
-        float c = b * range;
-        alpha[g] = a + c;
-        float e = lambda * beta_old;
-        float f = b * mn;
-        beta[g] = e + f;
-    }
-}
-
 // one workgroup per group: combine the partial extrema, then Eq. (6)-(7)
 // variant kEmaSymmetric: the extrema are replaced by -m and +m, m = max |x| = max(-min, max);
 // variant kEmaFixedBeta: the offset is beta_fixed, only alpha is a running estimate (of max - beta_fixed)

@@ -33,7 +33,10 @@ def lists(B, Nq, Nk, causal=False, window=0, docs=0, prefix=False, pad=False, st
     (1, 1, 1, {}), (3, 5, 5, dict(causal=True)), (2, 70, 70, dict(causal=True, window=9)), (2, 70, 70, dict(window=9)), (4, 33, 90, dict(causal=True, pad=True)),
     (4, 90, 33, dict(causal=True)), (5, 65, 65, dict(causal=True, prefix=True, pad=True)), (3, 300, 300, dict(docs=7)), (3, 300, 300, dict(causal=True, docs=40, prefix=True, window=30)),
     (4, 40, 100, dict(causal=True, docs=5, pad=True, start=(-20, 90))), (2, 7, 0, {}), (2, 1, 513, dict(causal=True, docs=500)), (2, 300, 300, dict(window=1)),
-    (3, 20, 50, dict(start=(-30, 60), window=5, docs=3, pad=True))])
+    (3, 20, 50, dict(start=(-30, 60), window=5, docs=3, pad=True)),
+    # documents within, across and over several of the stretches that a workgroup takes
+    (2, 3000, 3000, dict(docs=3)), (1, 2500, 5000, dict(causal=True, docs=900, pad=True)), (2, 2049, 2049, dict(docs=1500, causal=True)),
+    (2, 1500, 4000, dict(docs=2, start=(-700, 3500), window=600))])
 def test_bounds(B, Nq, Nk, kw):
     l = lists(B, Nq, Nk, **kw)
     seen = seen_matrix(Nq, Nk, B, **l)
