@@ -417,7 +417,7 @@ typedef struct mesa_qkv_heads {
  * Forward, one pass over x:  y (T, Hq+Hk, D) contiguous, of dt;  rstd (T, Hq+Hk) binary32 (what the backward takes; NULL
  * without a norm);  q (T, Hq+Hk+Hv, D) int8, codes of every head of x with alpha, beta as they are on entry, Eq. (3)-(4);
  * alpha, beta [Hq+Hk+Hv] then moved by this batch's extrema, Eq. (6)-(7) -- bit for bit mesa_quantize_update_fused on x with the
- * layout {T, Hq+Hk+Hv, D}.  Row t of x is at x + t*x_row elements (x_row a multiple of 8, >= (Hq+Hk+Hv)*D).
+ * layout {T, Hq+Hk+Hv, D}.  Row t of x is at x + t*x_row elements (x_row a multiple of 8, >= (Hq+Hk+Hv)*D, < 2^24).
  * gamma_q, gamma_k: [D] of dt.  freq: [rot/2] binary32.  pos: [axes][T] int32, any value.  x, y, q, gamma_* 16-byte aligned.
  * ws: mesa_qkv_norm_rope_fwd_q_workspace_bytes(h, dt) bytes.
  */
@@ -435,7 +435,7 @@ mesa_status mesa_qkv_norm_rope_recompute_q(const int8_t *q, mesa_qkv_heads h, co
  *   dx = rstd * (u - n * mean_d(u*n)),   dgamma_q[d] = sum over tokens and query heads of g*n, dgamma_k likewise
  * (without a norm dx = g; q, alpha, beta, rstd, dgamma_* are not used and may be NULL).
  * dy (T, Hq+Hk, D) contiguous of dt.  Row t of dx is at dx + t*dx_row elements, Hq+Hk heads (dx_row a multiple of 8,
- * >= (Hq+Hk)*D): rows of the projection's gradient, whose value heads stay as they are.  dx may alias dy where its rows are
+ * >= (Hq+Hk)*D, < 2^24): rows of the projection's gradient, whose value heads stay as they are.  dx may alias dy where its rows are
  * dy's.  dgamma_*: [D] binary32, overwritten, fixed summation order.  ws: mesa_qkv_norm_rope_bwd_q_workspace_bytes(h, dt) bytes.
  */
 size_t mesa_qkv_norm_rope_bwd_q_workspace_bytes(mesa_qkv_heads h, mesa_dtype dt);

@@ -30,6 +30,8 @@ struct QkvGeom {
     uint32_t Hq, Hn, H, D, rot, lph_log2;   // Hn = Hq + Hk, H = Hn + Hv
     uint32_t tile, phases_log2;             // tokens per tile; into how many parts the four waves share out a tile's tokens
     uint32_t end[4];                        // first pair behind each axis
+    uint32_t parts, angles;                 // lanes that hold pairs to turn; angles of a token in LDS
+    FastDiv div_half;
     int interleaved;
     float eps;
 };
@@ -59,6 +61,10 @@ static QkvGeom qkv_geom(const mesa_qkv_heads &h)
         g.end[a] = a < h.axes - 1 ? e : 0xFFFFFFFFu;
     }
     g.interleaved = h.interleaved;
+    const uint32_t per = h.interleaved ? 4 : 8;
+    g.parts = (g.rot / 2 + per - 1) / per;
+    g.angles = g.parts * per;
+    g.div_half = make_fastdiv(g.rot ? g.rot / 2 : 1);
     g.eps = h.eps;
     return g;
 }
@@ -69,55 +75,93 @@ static int qkv_grid(const QkvGeom &g)
     return int(n < kQkvGrid ? n : kQkvGrid);
 }
 
-// cosines and sines of a tile's tokens, [token][pair]
+// cosines and sines of a tile's tokens.  A lane reads those of its own part of a head in 16-byte pieces of two pairs, and the pieces of
+// neighbouring lanes lie side by side: pair i of a token is at [token][(i % per) / 2][i / per][i % 2], per pairs to a lane (side
+// by side in a lane's own order the pieces lay 64 bytes apart and met in a quarter of the banks).
+__device__ __forceinline__ uint32_t qkv_pair_at(const QkvGeom &g, uint32_t lane_part, uint32_t k)   // of a lane's pair k
+{
+    return ((k >> 1) * g.parts + lane_part) * 2 + (k & 1);
+}
 __device__ __forceinline__ void qkv_angles(float2 *cs, const QkvGeom &g, const float *__restrict__ freq, const int32_t *__restrict__ pos, int64_t t0, uint32_t tokens)
 {
-    const uint32_t half = g.rot / 2;
+    const uint32_t half = g.rot / 2, per_log2 = g.interleaved ? 2 : 3;
     for (uint32_t k = threadIdx.x; k < tokens * half; k += kThreads) {
-        const uint32_t tk = k / half, i = k - tk * half;
+        const uint32_t tk = fastdiv(k, g.div_half), i = k - tk * half;
         const uint32_t axis = (i >= g.end[0]) + (i >= g.end[1]) + (i >= g.end[2]);
         // in turns, the whole ones taken off: what is left is below a half and exact enough in binary32 (2^-25 turns)
         double turns = double(pos[int64_t(axis) * g.T + t0 + tk]) * double(freq[i]) * 0.15915494309189535;
         turns -= rint(turns);
         float s, c;
         sincospif(float(2.0 * turns), &s, &c);
-        cs[k] = make_float2(c, s);
+        cs[tk * g.angles + qkv_pair_at(g, i >> per_log2, i & ((1u << per_log2) - 1))] = make_float2(c, s);
+    }
+}
+
+// The other half of each pair, from the lane `hop` further on or back, by data-parallel-primitive moves where the hop is a power of two
+// below 16 (the LDS crossbar, which serves the whole compute unit, was what bound the backward: 250 -> FIGURE us at 32768 x 40 heads of 128).
+template <int CTRL, int BANKS> __device__ __forceinline__ float qkv_move(float old, float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, old), __builtin_bit_cast(int, v), CTRL, 0xf, BANKS, false));
+}
+__device__ __forceinline__ void qkv_partner(const float f[8], float o[8], uint32_t hop, int partner)
+{
+    if (hop == 8) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] = qkv_move<0x128, 0xf>(f[k], f[k]);                              // row_ror:8
+    } else if (hop == 4) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] = qkv_move<0x114, 0xa>(qkv_move<0x104, 0x5>(f[k], f[k]), f[k]);  // row_shl:4 and row_shr:4, each to every other four lanes
+    } else if (hop == 2) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] = qkv_move<0x4E, 0xf>(f[k], f[k]);                               // quad_perm [2,3,0,1]
+    } else if (hop == 1) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] = qkv_move<0xB1, 0xf>(f[k], f[k]);                               // quad_perm [1,0,3,2]
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] = __shfl(f[k], partner, 64);
     }
 }
 
 // f[0..7] of this lane's part of a head, turned by the token's angles; d0: the part's first element.  sign -1: turned back.
 // Every lane of the wave takes part (the partner's elements come from its registers).
-__device__ __forceinline__ void qkv_turn(float f[8], const float2 *cs, uint32_t d0, uint32_t rot, int interleaved, int partner, float sign)
+__device__ __forceinline__ void qkv_turn(float f[8], const float2 *cs, const QkvGeom &g, uint32_t d0, int partner, float sign)
 {
-    if (interleaved) {
+    if (g.interleaved) {
+        const uint32_t part = d0 / 8 < g.parts ? d0 / 8 : 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t i = d0 / 2 + k;
-            if (2 * i < rot) {
-                const float2 w = cs[i];
-                const float a = f[2 * k], b = f[2 * k + 1], s = sign * w.y;
-                f[2 * k] = fmaf(a, w.x, -(b * s));
-                f[2 * k + 1] = fmaf(b, w.x, a * s);
-            }
+            const float2 w = cs[qkv_pair_at(g, part, k)];
+            const float a = f[2 * k], b = f[2 * k + 1], s = sign * w.y;
+            const bool turned = d0 + 2 * k < g.rot;
+            f[2 * k] = turned ? fmaf(a, w.x, -(b * s)) : a;
+            f[2 * k + 1] = turned ? fmaf(b, w.x, a * s) : b;
         }
         return;
     }
-    const bool second = d0 >= rot / 2, turned = d0 < rot;
-    const float2 *p = cs + (turned ? (second ? d0 - rot / 2 : d0) : 0);
+    const bool second = d0 >= g.rot / 2, turned = d0 < g.rot;
+    const uint32_t part = turned ? (second ? d0 - g.rot / 2 : d0) / 8 : 0;
     const float sg = second ? sign : -sign;
+    float o[8];
+    qkv_partner(f, o, g.rot / 16, partner);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const float other = __shfl(f[k], partner, 64);
-        const float2 w = p[k];
-        const float v = fmaf(f[k], w.x, other * (sg * w.y));
+        const float2 w = cs[qkv_pair_at(g, part, k)];
+        const float v = fmaf(f[k], w.x, o[k] * (sg * w.y));
         f[k] = turned ? v : f[k];
     }
 }
 
-__device__ __forceinline__ float qkv_head_sum(float v, uint32_t lph_log2)
+__device__ __forceinline__ float qkv_head_sum(float v, uint32_t lph_log2)      // over the lanes of a head
 {
-    for (uint32_t k = 0; k < lph_log2; ++k) v += __shfl_xor(v, 1 << k, 64);
-    return v;
+    switch (lph_log2) {
+    case 0: return v;
+    case 1: return v + dpp_move<0xB1>(v);
+    case 2: return lanes_sum_dpp<4>(v);
+    case 3: return lanes_sum_dpp<8>(v);
+    case 4: return lanes_sum_dpp<16>(v);
+    }
+    return lanes_sum_dpp<32>(v);
 }
 
 __device__ __forceinline__ void qkv_hat(u32x2 c, float s, float b, float f[8])
@@ -128,23 +172,26 @@ __device__ __forceinline__ void qkv_hat(u32x2 c, float s, float b, float f[8])
 }
 
 // The forward (AGAIN false: from x, with codes and extrema) or queries and keys once more (AGAIN: from the codes and rstd).
-// Both round y once, from binary32.
+// Both round y once, from binary32.  Lanes without an element and tokens past the tile lie outside of their spans: no access is
+// conditional.
 template <typename T, bool SR, bool AGAIN>
-__global__ __launch_bounds__(kThreads) void k_qkv_fwd(QkvGeom g, const void *__restrict__ x, int64_t x_row, const int8_t *__restrict__ qin, const void *__restrict__ gamma_q,
+__global__ __launch_bounds__(kThreads, 4) void k_qkv_fwd(QkvGeom g, const void *__restrict__ x, int64_t x_row, const int8_t *__restrict__ qin, const void *__restrict__ gamma_q,
                                                       const void *__restrict__ gamma_k, const float *__restrict__ freq, const int32_t *__restrict__ pos,
                                                       float *alpha, float *beta, float lambda, void *__restrict__ y, float *__restrict__ rstd,
                                                       int8_t *__restrict__ q, uint64_t seed, uint64_t offset, float *__restrict__ part)
 {
     typedef typename Store<T>::raw_t Raw;
+    constexpr uint32_t kEb = sizeof(T);
     extern __shared__ float2 smem[];
     float2 *cs = smem;
-    int *lmn = reinterpret_cast<int *>(smem + g.tile * (g.rot / 2)), *lmx = lmn + g.H;
+    int *lmn = reinterpret_cast<int *>(smem + g.tile * g.angles), *lmx = lmn + g.H;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     const uint32_t lph = 1u << g.lph_log2, hpw = 64u >> g.lph_log2;
     const uint32_t d0 = (lane & (lph - 1)) * 8, sub = lane >> g.lph_log2;
     const int hop = int(g.rot / 16), partner = int(lane) + (d0 < g.rot / 2 ? hop : d0 < g.rot ? -hop : 0);
     const uint32_t heads = AGAIN ? g.Hn : g.H, slots = (heads + hpw - 1) / hpw;
     const uint32_t phase = wave & ((1u << g.phases_log2) - 1), phases = 1u << g.phases_log2;
+    const uint32_t wide = g.H * g.D, slim = g.Hn * g.D;       // elements of a token: codes; y
     const float inv_d = 1.0f / float(g.D);
     if (!AGAIN)
         for (uint32_t h = threadIdx.x; h < g.H; h += kThreads) {
@@ -153,13 +200,16 @@ __global__ __launch_bounds__(kThreads) void k_qkv_fwd(QkvGeom g, const void *__r
         }
     for (int64_t t0 = int64_t(blockIdx.x) * g.tile; t0 < g.T; t0 += int64_t(gridDim.x) * g.tile) {
         const uint32_t tokens = g.T - t0 < g.tile ? uint32_t(g.T - t0) : g.tile;
+        const Span sx(AGAIN ? nullptr : static_cast<const char *>(x) + t0 * x_row * kEb, AGAIN ? 0 : kNowhere), sq((AGAIN ? qin : q) + t0 * wide, tokens * wide);
+        const Span sy(static_cast<char *>(y) + t0 * slim * kEb, tokens * slim * kEb), sr(rstd ? rstd + t0 * g.Hn : nullptr, rstd ? tokens * g.Hn * 4 : 0);
         __syncthreads();                           // the last tile's angles are done with
         qkv_angles(cs, g, freq, pos, t0, tokens);
         __syncthreads();
         for (uint32_t slot = wave >> g.phases_log2; slot < slots; slot += (kThreads / 64) >> g.phases_log2) {
             const uint32_t hd = slot * hpw + sub;
-            const bool act = hd < heads && d0 < g.D, turn = hd < g.Hn;
+            const bool act = hd < heads && d0 < g.D, turn = act && hd < g.Hn;
             const bool any_turn = slot * hpw < g.Hn;     // uniform
+            const uint32_t at = hd * g.D + d0;
             float r = 0.0f, b = 0.0f, gam[8];
             if (act) {
                 b = beta[hd];
@@ -168,7 +218,7 @@ __global__ __launch_bounds__(kThreads) void k_qkv_fwd(QkvGeom g, const void *__r
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k) gam[k] = 1.0f;
-            if (gamma_q && act && turn) Store<T>::unpack(Store<T>::load(hd < g.Hq ? gamma_q : gamma_k, d0), gam);
+            if (gamma_q && turn) Store<T>::unpack(Store<T>::load(hd < g.Hq ? gamma_q : gamma_k, d0), gam);
             float mn = __builtin_inff(), mx = -__builtin_inff();
             for (uint32_t base = phase; base < tokens; base += phases * kQkvU) {
                 Raw raw[kQkvU];
@@ -177,19 +227,19 @@ __global__ __launch_bounds__(kThreads) void k_qkv_fwd(QkvGeom g, const void *__r
 #pragma unroll
                 for (int u = 0; u < kQkvU; ++u) {
                     const uint32_t tk = base + u * phases;
-                    const int64_t t = t0 + (tk < tokens ? tk : base);       // past the tile: its first token again, not stored
+                    const bool live = act && tk < tokens;
                     if (AGAIN) {
-                        cin[u] = act ? nt_load<u32x2>(qin + (t * g.H + hd) * g.D + d0) : u32x2{0u, 0u};
-                        rs[u] = gamma_q && act ? rstd[t * g.Hn + hd] : 1.0f;
+                        cin[u] = sq.load8(live ? tk * wide + at : kNowhere);
+                        rs[u] = gamma_q ? sr.load_f32(live ? (tk * g.Hn + hd) * 4 : kNowhere) : 1.0f;
                     } else {
-                        raw[u] = act ? Nt<T>::load(x, t * x_row + int64_t(hd) * g.D + d0) : Raw{};
+                        // past the tile: its first token again, so that extrema stay what they are
+                        sx.load(act ? ((tk < tokens ? tk : base) * uint32_t(x_row) + at) * kEb : kNowhere, raw[u]);
                     }
                 }
 #pragma unroll
                 for (int u = 0; u < kQkvU; ++u) {
                     const uint32_t tk = base + u * phases;
                     const bool live = act && tk < tokens;
-                    const int64_t t = t0 + (tk < tokens ? tk : base);
                     float f[8];
                     if (AGAIN) {
                         qkv_hat(cin[u], r, b, f);
@@ -197,9 +247,9 @@ __global__ __launch_bounds__(kThreads) void k_qkv_fwd(QkvGeom g, const void *__r
                         for (int k = 0; k < 8; ++k) f[k] *= rs[u] * gam[k];
                     } else {
                         Store<T>::unpack(raw[u], f);
-                        const int64_t e = (t * g.H + hd) * g.D + d0;
+                        const uint32_t e = tk * wide + at;
                         float v[8], bits[8];
-                        if (SR) sr_bits(seed, offset + uint64_t(e >> 3), bits);
+                        if (SR) sr_bits(seed, offset + uint64_t((t0 * wide + e) >> 3), bits);
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
                             v[k] = quantize_real<SR>(f[k], r, b, SR ? bits[k] : 0.0f);
@@ -207,20 +257,20 @@ __global__ __launch_bounds__(kThreads) void k_qkv_fwd(QkvGeom g, const void *__r
                             mx = vmax(mx, f[k]);
                         }
                         const u32x2 c = round_pack_codes<SR>(v);
-                        if (live) nt_store<u32x2>(q + e, c);
+                        sq.store8(live ? e : kNowhere, c);
                         if (!any_turn) continue;
                         if (gamma_q) {
                             float ss = 0.0f;
 #pragma unroll
                             for (int k = 0; k < 8; ++k) ss = fmaf(f[k], f[k], ss);
                             const float rr = 1.0f / sqrtf(fmaf(qkv_head_sum(ss, g.lph_log2), inv_d, g.eps));
-                            if (live && turn && d0 == 0) rstd[t * g.Hn + hd] = rr;
+                            sr.store_f32(live && turn && d0 == 0 ? (tk * g.Hn + hd) * 4 : kNowhere, rr);
 #pragma unroll
                             for (int k = 0; k < 8; ++k) f[k] *= rr * gam[k];
                         }
                     }
-                    if (g.rot) qkv_turn(f, cs + (tk < tokens ? tk : base) * (g.rot / 2), d0, g.rot, g.interleaved, partner, 1.0f);
-                    if (live && turn) Nt<T>::store(y, (t * g.Hn + hd) * g.D + d0, Store<T>::pack(f));
+                    if (g.rot) qkv_turn(f, cs + (tk < tokens ? tk : 0) * g.angles, g, d0, partner, 1.0f);
+                    sy.store(live && turn ? (tk * slim + at) * kEb : kNowhere, Store<T>::pack(f));
                 }
             }
             if (!AGAIN && act) {
@@ -245,12 +295,13 @@ __global__ __launch_bounds__(kThreads) void k_qkv_fwd(QkvGeom g, const void *__r
 
 // The backward; part[workgroup][2][D] takes the gains' gradients of its tokens, of query heads and of key heads.
 template <typename T, bool NORM>
-__global__ __launch_bounds__(kThreads) void k_qkv_bwd(QkvGeom g, const int8_t *__restrict__ q, const void *__restrict__ gamma_q, const void *__restrict__ gamma_k,
+__global__ __launch_bounds__(kThreads, NORM ? 3 : 4) void k_qkv_bwd(QkvGeom g, const int8_t *__restrict__ q, const void *__restrict__ gamma_q, const void *__restrict__ gamma_k,
                                                       const float *__restrict__ freq, const int32_t *__restrict__ pos, const float *__restrict__ alpha,
                                                       const float *__restrict__ beta, const float *__restrict__ rstd, const void *dy, void *dx, int64_t dx_row,
                                                       float *__restrict__ part, float *__restrict__ dgamma_q, float *__restrict__ dgamma_k)
 {
     typedef typename Store<T>::raw_t Raw;
+    constexpr uint32_t kEb = sizeof(T);
     extern __shared__ float2 smem[];
     float2 *cs = smem;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
@@ -259,18 +310,22 @@ __global__ __launch_bounds__(kThreads) void k_qkv_bwd(QkvGeom g, const int8_t *_
     const int hop = int(g.rot / 16), partner = int(lane) + (d0 < g.rot / 2 ? hop : d0 < g.rot ? -hop : 0);
     const uint32_t slots = (g.Hn + hpw - 1) / hpw;
     const uint32_t phase = wave & ((1u << g.phases_log2) - 1), phases = 1u << g.phases_log2;
+    const uint32_t wide = g.H * g.D, slim = g.Hn * g.D;
     const float inv_d = 1.0f / float(g.D);
     float acc[2][8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) acc[0][k] = acc[1][k] = 0.0f;
     for (int64_t t0 = int64_t(blockIdx.x) * g.tile; t0 < g.T; t0 += int64_t(gridDim.x) * g.tile) {
         const uint32_t tokens = g.T - t0 < g.tile ? uint32_t(g.T - t0) : g.tile;
+        const Span sdy(static_cast<const char *>(dy) + t0 * slim * kEb, tokens * slim * kEb), sdx(static_cast<char *>(dx) + t0 * dx_row * kEb, kNowhere);
+        const Span sq(NORM ? q + t0 * wide : nullptr, NORM ? tokens * wide : 0), sr(NORM ? rstd + t0 * g.Hn : nullptr, NORM ? tokens * g.Hn * 4 : 0);
         __syncthreads();
         qkv_angles(cs, g, freq, pos, t0, tokens);
         __syncthreads();
         for (uint32_t slot = wave >> g.phases_log2; slot < slots; slot += (kThreads / 64) >> g.phases_log2) {
             const uint32_t hd = slot * hpw + sub;
             const bool act = hd < g.Hn && d0 < g.D, key = hd >= g.Hq;
+            const uint32_t at = hd * g.D + d0;
             float s = 0.0f, b = 0.0f, gam[8];
             if (NORM && act) {
                 s = alpha[hd] / 255.0f;
@@ -289,36 +344,35 @@ __global__ __launch_bounds__(kThreads) void k_qkv_bwd(QkvGeom g, const int8_t *_
 #pragma unroll
                 for (int u = 0; u < kQkvU; ++u) {
                     const uint32_t tk = base + u * phases;
-                    const int64_t t = t0 + (tk < tokens ? tk : base);
-                    raw[u] = act ? Nt<T>::load(dy, (t * g.Hn + hd) * g.D + d0) : Raw{};
+                    const bool live = act && tk < tokens;
+                    sdy.load(live ? (tk * slim + at) * kEb : kNowhere, raw[u]);
                     if (NORM) {
-                        cin[u] = act ? nt_load<u32x2>(q + (t * g.H + hd) * g.D + d0) : u32x2{0u, 0u};
-                        rs[u] = act ? rstd[t * g.Hn + hd] : 0.0f;
+                        cin[u] = sq.load8(live ? tk * wide + at : kNowhere);
+                        rs[u] = sr.load_f32(live ? (tk * g.Hn + hd) * 4 : kNowhere);
                     }
                 }
 #pragma unroll
                 for (int u = 0; u < kQkvU; ++u) {
                     const uint32_t tk = base + u * phases;
                     const bool live = act && tk < tokens;
-                    const int64_t t = t0 + (tk < tokens ? tk : base);
                     float f[8];
-                    Store<T>::unpack(raw[u], f);
-                    if (g.rot) qkv_turn(f, cs + (tk < tokens ? tk : base) * (g.rot / 2), d0, g.rot, g.interleaved, partner, -1.0f);
+                    Store<T>::unpack(raw[u], f);           // zeros where nothing was loaded
+                    if (g.rot) qkv_turn(f, cs + (tk < tokens ? tk : 0) * g.angles, g, d0, partner, -1.0f);
                     if (NORM) {
                         float n[8], dot = 0.0f;
                         qkv_hat(cin[u], s, b, n);
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
                             n[k] *= rs[u];
-                            if (live) mine[k] = fmaf(f[k], n[k], mine[k]);
+                            mine[k] = fmaf(f[k], n[k], mine[k]);
                             f[k] *= gam[k];
                             dot = fmaf(f[k], n[k], dot);
                         }
-                        const float mean = qkv_head_sum(act ? dot : 0.0f, g.lph_log2) * inv_d;
+                        const float mean = qkv_head_sum(dot, g.lph_log2) * inv_d;
 #pragma unroll
                         for (int k = 0; k < 8; ++k) f[k] = rs[u] * fmaf(-n[k], mean, f[k]);
                     }
-                    if (live) Nt<T>::store(dx, t * dx_row + int64_t(hd) * g.D + d0, Store<T>::pack(f));
+                    sdx.store(live ? (tk * uint32_t(dx_row) + at) * kEb : kNowhere, Store<T>::pack(f));
                 }
             }
 #pragma unroll
@@ -387,7 +441,7 @@ static mesa_status check_qkv(const mesa_qkv_heads &h, mesa_dtype dt)
 
 static size_t qkv_lds(const QkvGeom &g, bool extrema)
 {
-    size_t n = size_t(g.tile) * (g.rot / 2) * 8 + (extrema ? size_t(g.H) * 8 : 0);
+    size_t n = size_t(g.tile) * g.angles * 8 + (extrema ? size_t(g.H) * 8 : 0);
     const size_t sums = size_t(8) * (8u << g.lph_log2) * 4;      // the backward's four waves
     return n > sums ? n : sums;
 }
@@ -419,7 +473,7 @@ extern "C" MESA_EXPORT mesa_status mesa_qkv_norm_rope_fwd_q(const void *x, int64
     if (const mesa_status st = check_qkv(h, dt)) return st;
     if (x_row % 8 != 0 || x_row < (h.Hq + h.Hk + h.Hv) * h.D || (gamma_q == nullptr) != (gamma_k == nullptr)) return MESA_ERR_INVALID_ARG;
     if (h.T == 0) return MESA_OK;
-    if (x_row >= (int64_t(1) << 31)) return MESA_ERR_UNSUPPORTED;
+    if (x_row >= (int64_t(1) << 24)) return MESA_ERR_UNSUPPORTED;
     if (!x || !y || !q || !alpha || !beta || x == y || !aligned16(x) || !aligned16(y) || !aligned16(q) || !aligned16(gamma_q) || !aligned16(gamma_k) || !aligned4(alpha) ||
         !aligned4(beta) || (gamma_q && !rstd) || !aligned4(rstd) || (h.rot && (!freq || !pos)) || !aligned4(freq) || !aligned4(pos))
         return MESA_ERR_INVALID_ARG;
@@ -470,7 +524,7 @@ extern "C" MESA_EXPORT mesa_status mesa_qkv_norm_rope_bwd_q(const int8_t *q, mes
     if (norm != (gamma_k != nullptr) || dx_row % 8 != 0 || dx_row < (h.Hq + h.Hk) * h.D || (norm && (!dgamma_q || !dgamma_k)) || !aligned4(dgamma_q) || !aligned4(dgamma_k))
         return MESA_ERR_INVALID_ARG;
     if (dx == dy && dx_row != (h.Hq + h.Hk) * h.D) return MESA_ERR_INVALID_ARG;
-    if (dx_row >= (int64_t(1) << 31)) return MESA_ERR_UNSUPPORTED;
+    if (dx_row >= (int64_t(1) << 24)) return MESA_ERR_UNSUPPORTED;
     if (h.T > 0) {
         if (!dy || !dx || !aligned16(dy) || !aligned16(dx) || (h.rot && (!freq || !pos)) || !aligned4(freq) || !aligned4(pos)) return MESA_ERR_INVALID_ARG;
         if (norm && (!q || !alpha || !beta || !rstd || !aligned16(q) || !aligned16(gamma_q) || !aligned16(gamma_k) || !aligned4(alpha) || !aligned4(beta) || !aligned4(rstd)))
