@@ -98,7 +98,7 @@ __device__ __forceinline__ void qkv_angles(float2 *cs, const QkvGeom &g, const f
 }
 
 // The other half of each pair, from the lane `hop` further on or back, by data-parallel-primitive moves where the hop is a power of two
-// below 16 (the LDS crossbar, which serves the whole compute unit, was what bound the backward: 250 -> FIGURE us at 32768 x 40 heads of 128).
+// below 16 (the LDS crossbar, which serves the whole compute unit, was what bound the backward: 250 -> 218 us at 32768 x 40 heads of 128).
 template <int CTRL, int BANKS> __device__ __forceinline__ float qkv_move(float old, float v)
 {
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, old), __builtin_bit_cast(int, v), CTRL, 0xf, BANKS, false));
@@ -295,13 +295,14 @@ __global__ __launch_bounds__(kThreads, 4) void k_qkv_fwd(QkvGeom g, const void *
 
 // The backward; part[workgroup][2][D] takes the gains' gradients of its tokens, of query heads and of key heads.
 template <typename T, bool NORM>
-__global__ __launch_bounds__(kThreads, NORM ? 3 : 4) void k_qkv_bwd(QkvGeom g, const int8_t *__restrict__ q, const void *__restrict__ gamma_q, const void *__restrict__ gamma_k,
+__global__ __launch_bounds__(kThreads, 4) void k_qkv_bwd(QkvGeom g, const int8_t *__restrict__ q, const void *__restrict__ gamma_q, const void *__restrict__ gamma_k,
                                                       const float *__restrict__ freq, const int32_t *__restrict__ pos, const float *__restrict__ alpha,
                                                       const float *__restrict__ beta, const float *__restrict__ rstd, const void *dy, void *dx, int64_t dx_row,
                                                       float *__restrict__ part, float *__restrict__ dgamma_q, float *__restrict__ dgamma_k)
 {
     typedef typename Store<T>::raw_t Raw;
     constexpr uint32_t kEb = sizeof(T);
+    constexpr int U = 2;                           // tokens in flight per wave: four took registers that the waves beside it need
     extern __shared__ float2 smem[];
     float2 *cs = smem;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
@@ -312,9 +313,11 @@ __global__ __launch_bounds__(kThreads, NORM ? 3 : 4) void k_qkv_bwd(QkvGeom g, c
     const uint32_t phase = wave & ((1u << g.phases_log2) - 1), phases = 1u << g.phases_log2;
     const uint32_t wide = g.H * g.D, slim = g.Hn * g.D;
     const float inv_d = 1.0f / float(g.D);
-    float acc[2][8];
+    // the gains' gradients of this lane's elements, of query and of key heads: in LDS, where only this lane reaches them
+    float *mine_q = reinterpret_cast<float *>(smem + g.tile * g.angles) + threadIdx.x * 8, *mine_k = mine_q + kThreads * 8;
+    if (NORM)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) acc[0][k] = acc[1][k] = 0.0f;
+        for (int k = 0; k < 8; ++k) mine_q[k] = mine_k[k] = 0.0f;
     for (int64_t t0 = int64_t(blockIdx.x) * g.tile; t0 < g.T; t0 += int64_t(gridDim.x) * g.tile) {
         const uint32_t tokens = g.T - t0 < g.tile ? uint32_t(g.T - t0) : g.tile;
         const Span sdy(static_cast<const char *>(dy) + t0 * slim * kEb, tokens * slim * kEb), sdx(static_cast<char *>(dx) + t0 * dx_row * kEb, kNowhere);
@@ -337,12 +340,12 @@ __global__ __launch_bounds__(kThreads, NORM ? 3 : 4) void k_qkv_bwd(QkvGeom g, c
             float mine[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) mine[k] = 0.0f;
-            for (uint32_t base = phase; base < tokens; base += phases * kQkvU) {
-                Raw raw[kQkvU];
-                u32x2 cin[kQkvU];
-                float rs[kQkvU];
+            for (uint32_t base = phase; base < tokens; base += phases * U) {
+                Raw raw[U];
+                u32x2 cin[U];
+                float rs[U];
 #pragma unroll
-                for (int u = 0; u < kQkvU; ++u) {
+                for (int u = 0; u < U; ++u) {
                     const uint32_t tk = base + u * phases;
                     const bool live = act && tk < tokens;
                     sdy.load(live ? (tk * slim + at) * kEb : kNowhere, raw[u]);
@@ -352,7 +355,7 @@ __global__ __launch_bounds__(kThreads, NORM ? 3 : 4) void k_qkv_bwd(QkvGeom g, c
                     }
                 }
 #pragma unroll
-                for (int u = 0; u < kQkvU; ++u) {
+                for (int u = 0; u < U; ++u) {
                     const uint32_t tk = base + u * phases;
                     const bool live = act && tk < tokens;
                     float f[8];
@@ -372,25 +375,25 @@ __global__ __launch_bounds__(kThreads, NORM ? 3 : 4) void k_qkv_bwd(QkvGeom g, c
 #pragma unroll
                         for (int k = 0; k < 8; ++k) f[k] = rs[u] * fmaf(-n[k], mean, f[k]);
                     }
+                    __builtin_amdgcn_sched_barrier(0);
                     sdx.store(live ? (tk * uint32_t(dx_row) + at) * kEb : kNowhere, Store<T>::pack(f));
                 }
             }
+            if (NORM) {
+                float *to = key ? mine_k : mine_q;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                acc[0][k] += key ? 0.0f : mine[k];
-                acc[1][k] += key ? mine[k] : 0.0f;
+                for (int k = 0; k < 8; ++k) to[k] += mine[k];
             }
         }
     }
     if (!NORM) return;
     // lanes that hold the same elements of different heads, then the four waves, each in a fixed order
-    float *sum = reinterpret_cast<float *>(smem);        // [wave][2][8 * lph]
-    __syncthreads();
+    float *sum = reinterpret_cast<float *>(smem + g.tile * g.angles) + 2 * kThreads * 8;        // [wave][2][8 * lph]
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            float v = acc[c][k];
+            float v = (c ? mine_k : mine_q)[k];
             for (uint32_t m = lph; m < 64; m <<= 1) v += __shfl_xor(v, int(m), 64);
             if (sub == 0) sum[((wave * 2 + c) << (g.lph_log2 + 3)) + d0 + k] = v;
         }
@@ -439,12 +442,8 @@ static mesa_status check_qkv(const mesa_qkv_heads &h, mesa_dtype dt)
     return MESA_OK;
 }
 
-static size_t qkv_lds(const QkvGeom &g, bool extrema)
-{
-    size_t n = size_t(g.tile) * g.angles * 8 + (extrema ? size_t(g.H) * 8 : 0);
-    const size_t sums = size_t(8) * (8u << g.lph_log2) * 4;      // the backward's four waves
-    return n > sums ? n : sums;
-}
+static size_t qkv_lds_fwd(const QkvGeom &g, bool extrema) { return size_t(g.tile) * g.angles * 8 + (extrema ? size_t(g.H) * 8 : 0); }
+static size_t qkv_lds_bwd(const QkvGeom &g, bool norm) { return size_t(g.tile) * g.angles * 8 + (norm ? 2 * kThreads * 32 + size_t(8) * (8u << g.lph_log2) * 4 : 0); }
 
 }  // namespace mesa
 
@@ -480,7 +479,7 @@ extern "C" MESA_EXPORT mesa_status mesa_qkv_norm_rope_fwd_q(const void *x, int64
     const QkvGeom g = qkv_geom(h);
     const int grid = qkv_grid(g);
     if (!ws || !aligned4(ws) || ws_bytes < mesa_qkv_norm_rope_fwd_q_workspace_bytes(h, dt)) return MESA_ERR_WORKSPACE;
-    const size_t lds = qkv_lds(g, true);
+    const size_t lds = qkv_lds_fwd(g, true);
     hipStream_t s = static_cast<hipStream_t>(stream);
 #define MESA_QKV(T) \
     do { \
@@ -506,7 +505,7 @@ extern "C" MESA_EXPORT mesa_status mesa_qkv_norm_rope_recompute_q(const int8_t *
         (gamma_q && !rstd) || !aligned4(rstd) || (h.rot && (!freq || !pos)) || !aligned4(freq) || !aligned4(pos))
         return MESA_ERR_INVALID_ARG;
     const QkvGeom g = qkv_geom(h);
-    const size_t lds = qkv_lds(g, false);
+    const size_t lds = qkv_lds_fwd(g, false);
 #define MESA_QKV(T) \
     hipLaunchKernelGGL((k_qkv_fwd<T, false, true>), dim3(qkv_grid(g)), dim3(kThreads), lds, static_cast<hipStream_t>(stream), g, nullptr, 0, q, gamma_q, gamma_k, freq, pos, \
                        const_cast<float *>(alpha), const_cast<float *>(beta), 0.0f, y, const_cast<float *>(rstd), nullptr, 0, 0, nullptr)
@@ -534,7 +533,7 @@ extern "C" MESA_EXPORT mesa_status mesa_qkv_norm_rope_bwd_q(const int8_t *q, mes
     const QkvGeom g = qkv_geom(h);
     const int grid = qkv_grid(g);
     if (norm && (!ws || !aligned4(ws) || ws_bytes < mesa_qkv_norm_rope_bwd_q_workspace_bytes(h, dt))) return MESA_ERR_WORKSPACE;
-    const size_t lds = qkv_lds(g, false);
+    const size_t lds = qkv_lds_bwd(g, norm);
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (h.T > 0) {
 #define MESA_QKV(T) \
