@@ -341,37 +341,70 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : 2) void k_attn_fwd(const AtF
         }
 }
 
-// the splits of a row joined: weights 2^(lse_s - max), four elements per thread
+// The splits of a row joined, with weights 2^(lse_s - max): a workgroup per row, eight groups of 32 threads with four elements each
+// share out the splits and meet in LDS.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_attn_join(const AtFwd a, int64_t pieces)
+__global__ __launch_bounds__(kThreads) void k_attn_join(const AtFwd a)
 {
+    constexpr int kU = 4, kGroups = kThreads / 32;
     const AtShape &s = a.s;
-    const int64_t id = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-    if (id >= pieces) return;
-    const int quads = s.D / 4;
-    const int64_t at = id / quads;                       // (b, key head, row)
-    const int e = int(id - at * quads) * 4;
-    const int64_t step = int64_t(a.heads) * s.R;
-    float top = -__builtin_inff();
-    for (uint32_t k = 0; k < a.splits; ++k) top = fmaxf(top, a.part_lse[k * step + at]);
-    float total = 0.0f, x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (top > -__builtin_inff())
-        for (uint32_t k = 0; k < a.splits; ++k) {
-            const float w = at_exp2(a.part_lse[k * step + at] - top);
-            const float4 v = *reinterpret_cast<const float4 *>(a.part_o + (k * step + at) * s.D + e);
-            total += w;
-            x[0] = fmaf(w, v.x, x[0]);
-            x[1] = fmaf(w, v.y, x[1]);
-            x[2] = fmaf(w, v.z, x[2]);
-            x[3] = fmaf(w, v.w, x[3]);
+    __shared__ float sums[kGroups][32][5];
+    __shared__ float tops[kGroups];
+    const int64_t at = blockIdx.x, step = int64_t(a.heads) * s.R;     // (b, key head, row)
+    const int quad = threadIdx.x & 31, group = threadIdx.x >> 5, e = quad * 4;
+    const bool act = e < s.D;
+    float top = kAtLow, total = 0.0f, x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k0 = group; k0 < int(a.splits); k0 += kGroups * kU) {
+        float z[kU];
+        float4 v[kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {                                // four requested together; behind the last one this group's first again, without weight
+            const int64_t k = (k0 + u * kGroups < int(a.splits) ? k0 + u * kGroups : k0) * step + at;
+            z[u] = a.part_lse[k];
+            v[u] = act ? *reinterpret_cast<const float4 *>(a.part_o + k * s.D + e) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
+        float m = top;
+#pragma unroll
+        for (int u = 0; u < kU; ++u) m = fmaxf(m, z[u]);
+        const float f = at_exp2(top - m);
+        top = m;
+        total *= f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] *= f;
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            const float w = k0 + u * kGroups < int(a.splits) ? at_exp2(z[u] - m) : 0.0f;      // a split that saw nothing: -infinity, no weight
+            total += w;
+            x[0] = fmaf(w, v[u].x, x[0]);
+            x[1] = fmaf(w, v[u].y, x[1]);
+            x[2] = fmaf(w, v[u].z, x[2]);
+            x[3] = fmaf(w, v[u].w, x[3]);
+        }
+    }
+    if (quad == 0) tops[group] = top;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sums[group][quad][k] = x[k];
+    sums[group][quad][4] = total;
+    __syncthreads();
+    if (group > 0 || !act) return;
+    float m = kAtLow;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) m = fmaxf(m, tops[g]);
+    total = x[0] = x[1] = x[2] = x[3] = 0.0f;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        const float w = at_exp2(tops[g] - m);
+        total = fmaf(w, sums[g][quad][4], total);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = fmaf(w, sums[g][quad][k], x[k]);
+    }
     const float inv = total > 0.0f ? 1.0f / total : 0.0f;
     const uint32_t head = uint32_t(at / s.R), r = uint32_t(at - int64_t(head) * s.R);
     const int b = int(head) / s.Hk, hk = int(head) - b * s.Hk;
     const AtRow row = at_row(s, r);
     const int hq = hk * s.G + int(row.g);
     at_store4<T>(a.o.p + int64_t(b) * a.o.batch + int64_t(row.token) * a.o.token + int64_t(hq) * a.o.head + e * 2, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-    if (e == 0) a.lse[(int64_t(b) * s.Hq + hq) * s.Nq + row.token] = total > 0.0f ? (top + __log2f(total)) * kLn2 : -__builtin_inff();
+    if (e == 0) a.lse[(int64_t(b) * s.Hq + hq) * s.Nq + row.token] = total > 0.0f ? (m + __log2f(total)) * kLn2 : -__builtin_inff();
 }
 
 struct AtFwdPlan {
@@ -388,10 +421,14 @@ static AtFwdPlan at_fwd_plan(const mesa_attention &a)
     p.waves = R <= 32 ? 1 : 4;
     p.keys = p.waves == 1 ? 32 : 64;
     p.row_blocks = uint32_t(ceil_div(R, p.waves * 32));
-    const int64_t have = heads * p.row_blocks, want = p.waves == 1 ? 1536 : 384, most = a.Nk / (p.waves == 1 ? 256 : 512);
-    int64_t n = have > 0 ? want / have : 1;
+    // One wave per SIMD fits the wide heads' registers: 1024 workgroups at a time.  Two rounds of them even out lengths that differ (16 x 4
+    // heads over 16381 keys or fewer: 24 splits 90 us, 32 85, 64 88); with less than 256 keys each the rounds' own cost takes more
+    // than that (3001 keys: 23 splits 21.7 us, 16 17.5).
+    const int64_t have = heads * p.row_blocks, most = a.Nk / (p.waves == 1 ? 128 : 512);
+    int64_t n = have > 0 ? (p.waves == 1 ? 2048 : 384) / have : 1;
+    if (p.waves == 1 && n * 256 > a.Nk) n = 1024 / have;
     n = n > most ? most : n;
-    n = n > 64 ? 64 : n < 1 ? 1 : n;
+    n = n > 128 ? 128 : n < 1 ? 1 : n;
     p.splits = uint32_t(n);
     p.ws = n > 1 ? size_t(n) * size_t(heads) * size_t(R) * size_t(a.D + 1) * sizeof(float) : 0;
     return p;
@@ -471,7 +508,7 @@ extern "C" MESA_EXPORT mesa_status mesa_attention_fwd(mesa_attention a, mesa_att
         return MESA_ERR_INVALID_ARG;
     const AtFwdPlan p = at_fwd_plan(a);
     const int64_t groups = a.B * a.Hk, quads = groups * a.Nq * group * (a.D / 4);
-    if (groups * p.row_blocks * p.splits > most_workgroups(256) || ceil_div(quads, kThreads) > most_workgroups(kThreads)) return MESA_ERR_UNSUPPORTED;
+    if (groups * p.row_blocks * p.splits > most_workgroups(256) || (p.splits > 1 && groups * a.Nq * group > most_workgroups(kThreads)) || ceil_div(quads, kThreads) > most_workgroups(kThreads)) return MESA_ERR_UNSUPPORTED;
     if (p.ws && (!ws || !aligned16(ws) || ws_bytes < p.ws)) return MESA_ERR_WORKSPACE;
     hipStream_t s = static_cast<hipStream_t>(stream);
     AtFwd f;
@@ -499,8 +536,8 @@ extern "C" MESA_EXPORT mesa_status mesa_attention_fwd(mesa_attention a, mesa_att
     else a.D <= 64 ? at_fwd_forms<__bf16, 64>(f, p, cap, bias, s) : at_fwd_forms<__bf16, 128>(f, p, cap, bias, s);
     if (const mesa_status st = launch_status()) return st;
     if (p.splits > 1) {
-        if (half) hipLaunchKernelGGL(k_attn_join<_Float16>, flat, dim3(kThreads), 0, s, f, quads);
-        else hipLaunchKernelGGL(k_attn_join<__bf16>, flat, dim3(kThreads), 0, s, f, quads);
+        if (half) hipLaunchKernelGGL(k_attn_join<_Float16>, dim3(uint32_t(groups * f.s.R)), dim3(kThreads), 0, s, f);
+        else hipLaunchKernelGGL(k_attn_join<__bf16>, dim3(uint32_t(groups * f.s.R)), dim3(kThreads), 0, s, f);
         return launch_status();
     }
     return MESA_OK;
