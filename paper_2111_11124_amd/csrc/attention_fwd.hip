@@ -190,16 +190,14 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : 2) void k_attn_fwd(const AtF
     const float slope2 = BIAS ? s.slopes[hq] * kLog2e : 0.0f;
     const int place = BIAS ? at_place(s, b, row.token) : 0;
     __syncthreads();
-    int blo = 0x7FFFFFFF, bhi = 0, all_lo = 0, all_hi = 0x7FFFFFFF;      // the same of the workgroup's rows
+    int blo = 0x7FFFFFFF, bhi = 0, full_lo[NW], full_hi[NW];      // the same of the workgroup's rows; what each wave's rows see, all of them
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
         blo = range[0][w] < blo ? range[0][w] : blo;
         bhi = range[1][w] > bhi ? range[1][w] : bhi;
-        all_lo = range[2][w] > all_lo ? range[2][w] : all_lo;
-        all_hi = range[3][w] < all_hi ? range[3][w] : all_hi;
+        full_lo[w] = __builtin_amdgcn_readfirstlane(range[2][w]);
+        full_hi[w] = __builtin_amdgcn_readfirstlane(range[3][w]);
     }
-    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
-    all_hi = __builtin_amdgcn_readfirstlane(all_hi);
     int t0 = bhi > 0 ? blo / BN : 0, t1 = bhi > 0 ? (bhi + BN - 1) / BN : 0;
     if (a.splits > 1) {
         const int per = (t1 - t0 + int(a.splits) - 1) / int(a.splits);
@@ -302,7 +300,10 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : 2) void k_attn_fwd(const AtF
     for (int t = t0, cur = 0; t < t1; ++t, cur ^= 1) {
         char *lk = lds + cur * 2 * Tile::kBytes, *lv = lk + Tile::kBytes;
         const int j0 = t * BN;
-        if (j0 < all_lo || j0 + BN > all_hi) {
+        bool known = false;                         // some wave's rows see the whole tile: no key of it is unseen
+#pragma unroll
+        for (int w = 0; w < NW; ++w) known |= j0 >= full_lo[w] && j0 + BN <= full_hi[w];
+        if (!known) {
             const uint64_t some = at_seen<NW>(seen, wave, lane, j0, lo, hi);
             tk.keep(some);
             tv.keep(some);
