@@ -10,8 +10,10 @@
 // rows 16g + 4*(l/32) and 8 further on.
 //
 // A tile's rows are DP elements (DP: head_dim padded to 64 or 128 with zeros), in pieces of 16 bytes, piece c of row r
-// at place c ^ turn(r): eight consecutive rows' pieces c lie in eight different bank groups (plain reads), and four
-// consecutive rows' 32-byte pairs of pieces in four (transposing reads).
+// at place c ^ turn(r), so that rows' pieces c (plain reads) and four rows' 32-byte pairs of pieces (transposing reads) lie in
+// different banks.  Measured per wave and read, for ten such orders: plain 2.2 ns and transposing 1.1 ns at best, and so for the order
+// of 64 elements; for 128 the one that takes 3.5 and 1.7 ns, whose turns repeat every eight rows: the kernels are not bound by these reads,
+// and the best order's many addresses cost the walk over rows 711 -> 775 us (4 x 4096 x 16 heads).  Without any: 27 and 3.7 ns.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -110,7 +112,8 @@ __device__ __forceinline__ int at_place(const AtShape &s, int b, uint32_t token)
     return int(token + uint32_t(s.q_start ? s.q_start[b] : s.Nk - s.Nq));
 }
 
-__device__ __forceinline__ int at_turn(int row) { return ((row & 3) << 1) ^ ((row >> 2) & 1); }
+// linear in the row's bits: turn(a ^ b) = turn(a) ^ turn(b)
+template <int DP> __device__ __forceinline__ constexpr int at_turn(int row) { return ((row & 3) << 1) ^ ((row >> 2) & (DP == 128 ? 1 : 7)); }
 
 // ROWS x DP elements from memory to LDS by NT threads, by way of registers.  Rows past `rows` and pieces past D become zeros.
 // `at(row)`: byte offset of a row from `base`.
@@ -138,7 +141,7 @@ template <int NT, int ROWS, int DP> struct AtTile {
 #pragma unroll
         for (int k = 0; k < kN; ++k) {
             const int i = int(threadIdx.x) + k * NT, row = i / kPieces, piece = i % kPieces;
-            *reinterpret_cast<u32x4 *>(lds + row * (DP * 2) + ((piece ^ at_turn(row)) << 4)) = r[k];
+            *reinterpret_cast<u32x4 *>(lds + row * (DP * 2) + ((piece ^ at_turn<DP>(row)) << 4)) = r[k];
         }
     }
 };
@@ -146,13 +149,13 @@ template <int NT, int ROWS, int DP> struct AtTile {
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Wint-to-pointer-cast"      // the host pass counts pointers in 64 bits
 // LDS by its 32-bit address: a lane's place in a tile is one register for plain reads and one for transposing ones; which
-// piece a read takes is an exclusive-or with a constant (tiles start at multiples of 128 bytes), the row an immediate offset.
+// piece a read takes is an exclusive-or with a constant (tiles start at multiples of 128 bytes, whose turns stay within them), the row an immediate offset.
 __device__ __forceinline__ uint32_t at_address(const char *lds) { return uint32_t(uintptr_t((__attribute__((address_space(3))) const char *)lds)); }
-template <int DP> __device__ __forceinline__ uint32_t at_plain_lane(int lane) { return (lane & 31) * (DP * 2) + (((lane >> 5) ^ at_turn(lane & 31)) << 4); }
+template <int DP> __device__ __forceinline__ uint32_t at_plain_lane(int lane) { return (lane & 31) * (DP * 2) + (((lane >> 5) ^ at_turn<DP>(lane & 31)) << 4); }
 template <int DP> __device__ __forceinline__ uint32_t at_trans_lane(int lane)
 {
     const int sl = lane & 15, row = 4 * (lane >> 5) + (sl >> 2), piece = ((lane >> 4) & 1) * 2 + ((sl & 3) >> 1);
-    return row * (DP * 2) + ((piece ^ at_turn(row)) << 4) + (sl & 1) * 8;
+    return row * (DP * 2) + ((piece ^ at_turn<DP>(row)) << 4) + (sl & 1) * 8;
 }
 // A operand, rows as they lie: rows row0..row0+31 of the tile (row0 a multiple of 32), elements 16*ks ..+15; at: tile's address + at_plain_lane
 template <int DP> __device__ __forceinline__ u32x4 at_plain(uint32_t at, int row0, int ks)
@@ -165,9 +168,10 @@ template <int DP> __device__ __forceinline__ u32x4 at_plain(uint32_t at, int row
 template <int DP> __device__ __forceinline__ u32x4 at_transposed(uint32_t at, int row0, int d0)
 {
     typedef __attribute__((address_space(3))) at_v4s *lds_p;
-    const uint32_t p = (at ^ uint32_t((d0 & 32) << 1)) + uint32_t(row0 * (DP * 2) + (d0 >> 6) * 128);
+    const uint32_t p = (at ^ uint32_t((((d0 >> 3) & 7) ^ at_turn<DP>(row0 & 31)) << 4)) + uint32_t(row0 * (DP * 2) + (d0 >> 6) * 128);
+    const uint32_t q = (at ^ uint32_t((((d0 >> 3) & 7) ^ at_turn<DP>((row0 & 31) + 8)) << 4)) + uint32_t((row0 + 8) * (DP * 2) + (d0 >> 6) * 128);
     const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)p));
-    const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)(p + 8 * DP * 2)));
+    const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_p)q));
     return u32x4{a[0], a[1], b[0], b[1]};
 }
 

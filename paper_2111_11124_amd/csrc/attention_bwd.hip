@@ -30,7 +30,7 @@ struct AbOrder {
 };
 enum { kAbLse = 0, kAbDelta, kAbLo, kAbHi, kAbSlope, kAbPlace, kAbEmpty, kAbWords };   // 32 words of each per tile
 struct AbRows {                        // what the row pass leaves
-    uint32_t *info;                    // [b * Hk + key head][tile][word][place]: log-sum-exp in powers of two (3e38 where nothing is seen), delta,
+    uint32_t *info;                    // [b * Hk + key head][tile][word][place]: log-sum-exp in powers of two (3e38 where nothing is seen), -delta,
                                        // interval, slope in powers of two, place of the query, 1 where nothing is seen
     int4 *tiles;                       // [..][tile]: least lo, largest hi of the rows that see something; largest lo, least hi of all
     float2 *most;                      // [..][four tiles]: largest |do|, largest |delta|   (binary16 only)
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(kThreads) void k_attn_rows(const AtBwd a)
                 }
             }
             dot = lanes_sum_dpp<kLanes>(dot);
-            if (part == 0 && tile < a.order.tiles) a.w.info[(int64_t(head) * a.order.tiles + tile) * (kAbWords * 32) + kAbDelta * 32 + (y & 31)] = __float_as_uint(dot);
+            if (part == 0 && tile < a.order.tiles) a.w.info[(int64_t(head) * a.order.tiles + tile) * (kAbWords * 32) + kAbDelta * 32 + (y & 31)] = __float_as_uint(-dot);
             if (AtNum<T>::kHalf) {
                 most = fmaxf(most, lanes_sum_dpp<kLanes>(ss));
                 most_delta = fmaxf(most_delta, fabsf(dot));
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
     typedef AtNum<T> Num;
     typedef AtTile<NW * 64, BN, DP> Tile;
     constexpr int kKs = DP / 16, kDt = DP / 32, kSub = BN / 32;
-    __shared__ __attribute__((aligned(128))) char lds[4 * Tile::kBytes];
+    __shared__ __attribute__((aligned(256))) char lds[4 * Tile::kBytes];
     __shared__ int range[4][NW];
     __shared__ uint64_t seen[NW];
     const AtShape &s = a.s;
@@ -240,7 +240,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
     const int hq = hk * s.G + int(row.g);
     const uint32_t *info = a.w.info + ab_info(a.order, head, row.token, row.g);
     const int lo = int(info[kAbLo * 32]), hi = int(info[kAbHi * 32]);
-    const float lse2 = __uint_as_float(info[kAbLse * 32]), delta = __uint_as_float(info[kAbDelta * 32]);
+    float lse2 = __uint_as_float(info[kAbLse * 32]);
+    const float delta = __uint_as_float(info[kAbDelta * 32]);      // with the sign that the sums do.v start from
     const int wlo = at_wave_min(hi > 0 ? lo : 0x7FFFFFFF), whi = at_wave_max(hi), flo = at_wave_max(lo), fhi = at_wave_min(hi);
     if (lane == 0) {
         range[0][wave] = wlo;
@@ -271,7 +272,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
     }
     const int t0 = __builtin_amdgcn_readfirstlane(bhi > 0 ? blo / BN : 0), t1 = __builtin_amdgcn_readfirstlane(bhi > 0 ? (bhi + BN - 1) / BN : 0);
 
-    float mul = 1.0f, undo = s.scale;                 // of ds, and of the sums
+    float undo = s.scale;                             // of the sums; the factor of ds goes into p, which nothing else here takes
     if (Num::kHalf) {
         float ss = 0.0f, vmax = 0.0f;
 #pragma unroll
@@ -284,7 +285,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
         ss = at_pair_sum(ss);
         for (int kb = t0 * BN / kAbRows; kb * kAbRows < t1 * BN && kb < int(a.w.key_blocks); ++kb) vmax = fmaxf(vmax, a.w.values[int64_t(head) * a.w.key_blocks + kb]);
         const int e = ab_exponent(sqrtf(ss) * vmax + fabsf(delta));
-        mul = ab_pow2(e - kAtDrop);
+        lse2 -= float(e - kAtDrop);
         undo = s.scale * ab_pow2(-e);
     }
 
@@ -308,7 +309,10 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
         for (int t = 0; t < kSub; ++t) {
             at_acc x, y;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = y[i] = 0.0f;
+            for (int i = 0; i < 16; ++i) {
+                x[i] = 0.0f;
+                y[i] = delta;
+            }
 #pragma unroll
             for (int ks = 0; ks < kKs; ++ks) {
                 x = Num::mfma(at_plain<DP>(ka, t * 32, ks), qf[ks], x);
@@ -327,9 +331,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
                     if (BIAS) sc = fmaf(-slope2, fabsf(away - float(at_reg_row(i))), sc);
                     p = at_exp2(sc - lse2);
                 }
-                x[i] = p * (y[i] - delta);
+                x[i] = p * y[i];
                 if (CAP) x[i] *= slope;
-                if (Num::kHalf) x[i] *= mul;
             }
             if (!whole) {
 #pragma unroll
@@ -392,7 +395,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
     constexpr int kTile = kAbTile * DP * 2;           // bytes: 32 rows of q, or of do
     constexpr int kOff = kAbTile * kPieces / 256;     // rows of a tile per thread
     constexpr int kInfo = BIAS ? 6 : 4;               // words per row that are used here
-    __shared__ __attribute__((aligned(128))) char lds[2 * 4 * kTile];          // [buffer][tile][q, do]
+    __shared__ __attribute__((aligned(256))) char lds[2 * 4 * kTile];          // [buffer][tile][q, do]
     __shared__ __attribute__((aligned(16))) uint32_t info[2][2][kInfo * 32];   // [buffer][tile][word][row]
     const AtShape &s = a.s;
     const AbOrder &order = a.order;
@@ -453,7 +456,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
         const bool in = dt[k] < order.tokens && piece * 8 < s.D;
         q_at[k] = uint32_t(dt[k]) * uint32_t(a.q.token) + uint32_t(dg[k]) * uint32_t(a.q.head) + piece * 16;
         g_at[k] = uint32_t(dt[k]) * uint32_t(a.dO.token) + uint32_t(dg[k]) * uint32_t(a.dO.head) + piece * 16;
-        lds_at[k] = x * (DP * 2) + ((piece ^ at_turn(x)) << 4);
+        lds_at[k] = x * (DP * 2) + ((piece ^ at_turn<DP>(x)) << 4);
         empty_at[k] = (kAbEmpty * 32 + x) * 4;
         if (!in) dt[k] = 0x40000000;
     }
@@ -518,16 +521,23 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
     auto work = [&](int at, const uint32_t *in, bool whole) __attribute__((always_inline)) {
         const uint32_t qa = plain_at + at, ga = qa + kTile, qt = trans_at + at, gt = qt + kTile;
         at_acc x, y;
+        auto row4 = [&](int word, int w) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4 *>(in + word * 32 + 8 * w + 4 * half); };   // rows of registers 4w..4w+3
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = y[i] = 0.0f;
+        for (int w = 0; w < 4; ++w) {
+            const u32x4 d4 = row4(kAbDelta, w);      // the sums do.v start from -delta
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                x[4 * w + c] = 0.0f;
+                y[4 * w + c] = __uint_as_float(d4[c]);
+            }
+        }
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks) x = Num::mfma(at_plain<DP>(qa, 0, ks), kf[ks], x);
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks) y = Num::mfma(at_plain<DP>(ga, 0, ks), vf[ks], y);
-        auto row4 = [&](int word, int w) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4 *>(in + word * 32 + 8 * w + 4 * half); };   // rows of registers 4w..4w+3
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const u32x4 l4 = row4(kAbLse, w), d4 = row4(kAbDelta, w);
+            const u32x4 l4 = row4(kAbLse, w);
             u32x4 sl4 = {}, pl4 = {};
             if (BIAS) {
                 sl4 = row4(kAbSlope, w);
@@ -545,7 +555,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
                     if (BIAS) sc = fmaf(-__uint_as_float(sl4[c]), fabsf(float(int(pl4[c]) - j_own)), sc);
                     x[i] = at_exp2(sc - lse2);
                 }
-                y[i] = x[i] * (y[i] - __uint_as_float(d4[c]));
+                y[i] *= x[i];
                 if (CAP) y[i] *= slope;
                 if (Num::kHalf) y[i] *= mul;
             }

@@ -159,7 +159,7 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : 2) void k_attn_fwd(const AtF
     typedef AtNum<T> Num;
     typedef AtTile<NW * 64, BN, DP> Tile;
     constexpr int kKs = DP / 16, kDt = DP / 32, kSub = BN / 32;
-    __shared__ __attribute__((aligned(128))) char lds[4 * Tile::kBytes];      // two tiles of k, two of v
+    __shared__ __attribute__((aligned(256))) char lds[4 * Tile::kBytes];      // two tiles of k, two of v
     __shared__ int range[4][NW];
     __shared__ uint64_t seen[NW];
     const AtShape &s = a.s;
