@@ -520,45 +520,54 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
     const uint32_t plain_at = at_address(lds) + at_plain_lane<DP>(lane), trans_at = at_address(lds) + at_trans_lane<DP>(lane);
     auto work = [&](int at, const uint32_t *in, bool whole) __attribute__((always_inline)) {
         const uint32_t qa = plain_at + at, ga = qa + kTile, qt = trans_at + at, gt = qt + kTile;
+        // A wave issues in order, and at 128 elements it is alone on its SIMD: what is to run beside a product has to stand between
+        // products, and what a product reads has to be on its way well before.  Fences keep the order below: scores; do.v with the
+        // exponentials between its products and dv's operands read meanwhile; dv with ds between; dk.
+        constexpr int kPer = 16 / kKs;               // scores per product
         at_acc x, y;
+        float slope[CAP ? 16 : 1];
+        u32x4 fq[kKs], fg[kKs], p[2], ds[2];
         auto row4 = [&](int word, int w) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4 *>(in + word * 32 + 8 * w + 4 * half); };   // rows of registers 4w..4w+3
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const u32x4 d4 = row4(kAbDelta, w);      // the sums do.v start from -delta
+        for (int ks = 0; ks < kKs; ++ks) fq[ks] = at_plain<DP>(qa, 0, ks);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                x[4 * w + c] = 0.0f;
-                y[4 * w + c] = __uint_as_float(d4[c]);
+        for (int ks = 0; ks < kKs; ++ks) fg[ks] = at_plain<DP>(ga, 0, ks);
+        u32x4 l4[4], d4[4], sl4[BIAS ? 4 : 1], pl4[BIAS ? 4 : 1];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            d4[w] = row4(kAbDelta, w);
+            l4[w] = row4(kAbLse, w);
+            if (BIAS) {
+                sl4[w] = row4(kAbSlope, w);
+                pl4[w] = row4(kAbPlace, w);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int ks = 0; ks < kKs; ++ks) x = Num::mfma(at_plain<DP>(qa, 0, ks), kf[ks], x);
+        for (int i = 0; i < 16; ++i) {
+            x[i] = 0.0f;
+            y[i] = __uint_as_float(d4[i / 4][i % 4]);      // the sums do.v start from -delta
+        }
 #pragma unroll
-        for (int ks = 0; ks < kKs; ++ks) y = Num::mfma(at_plain<DP>(ga, 0, ks), vf[ks], y);
+        for (int ks = 0; ks < kKs; ++ks) x = Num::mfma(fq[ks], kf[ks], x);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const u32x4 l4 = row4(kAbLse, w);
-            u32x4 sl4 = {}, pl4 = {};
-            if (BIAS) {
-                sl4 = row4(kAbSlope, w);
-                pl4 = row4(kAbPlace, w);
-            }
+        for (int ks = 0; ks < kKs; ++ks) {
+            y = Num::mfma(fg[ks], vf[ks], y);
+            fq[ks] = at_transposed<DP>(gt, ks / kDt * 16, ks % kDt * 32);     // dv's operands, 2 * kDt = kKs of them
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int i = 4 * w + c;
-                const float lse2 = __uint_as_float(l4[c]);
-                float slope = 1.0f;
+            for (int i = ks * kPer; i < ks * kPer + kPer; ++i) {
+                const float lse2 = __uint_as_float(l4[i / 4][i % 4]);
                 if (!CAP && !BIAS) {
                     x[i] = at_exp2(fmaf(x[i], s.c, -lse2));
                 } else {
-                    float sc = ab_score<CAP>(s, x[i], slope);
-                    if (BIAS) sc = fmaf(-__uint_as_float(sl4[c]), fabsf(float(int(pl4[c]) - j_own)), sc);
+                    float sl = 1.0f, sc = ab_score<CAP>(s, x[i], sl);
+                    if (CAP) slope[i] = sl;
+                    if (BIAS) sc = fmaf(-__uint_as_float(sl4[i / 4][i % 4]), fabsf(float(int(pl4[i / 4][i % 4]) - j_own)), sc);
                     x[i] = at_exp2(sc - lse2);
                 }
-                y[i] *= x[i];
-                if (CAP) y[i] *= slope;
-                if (Num::kHalf) y[i] *= mul;
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
         if (!whole) {
 #pragma unroll
@@ -572,21 +581,27 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
                 }
             }
         }
-        u32x4 p[2], ds[2];
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                p[g][w] = Num::pack(x[8 * g + 2 * w], x[8 * g + 2 * w + 1]);
-                ds[g][w] = Num::pack(y[8 * g + 2 * w], y[8 * g + 2 * w + 1]);
+            for (int w = 0; w < 4; ++w) p[g][w] = Num::pack(x[8 * g + 2 * w], x[8 * g + 2 * w + 1]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < kKs; ++n) {
+            dv[n % kDt] = Num::mfma(fq[n], p[n / kDt], dv[n % kDt]);
+            fg[n] = at_transposed<DP>(qt, n / kDt * 16, n % kDt * 32);        // dk's operands
+#pragma unroll
+            for (int i = n * kPer; i < n * kPer + kPer; ++i) {
+                y[i] *= x[i];
+                if (CAP) y[i] *= slope[i];
+                if (Num::kHalf) y[i] *= mul;
             }
 #pragma unroll
-        for (int g = 0; g < 2; ++g)
+            for (int w = n * kPer / 2; w < (n + 1) * kPer / 2; ++w) ds[w / 4][w % 4] = Num::pack(y[2 * w], y[2 * w + 1]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
-            for (int d = 0; d < kDt; ++d) {
-                dv[d] = Num::mfma(at_transposed<DP>(gt, g * 16, d * 32), p[g], dv[d]);
-                dk[d] = Num::mfma(at_transposed<DP>(qt, g * 16, d * 32), ds[g], dk[d]);
-            }
+        for (int n = 0; n < kKs; ++n) dk[n % kDt] = Num::mfma(fg[n], ds[n / kDt], dk[n % kDt]);
     };
     int t = __builtin_amdgcn_readfirstlane(next());
     if (t >= 0) fetch(t);

@@ -154,7 +154,7 @@ struct AtFwd {
 
 // NW waves of 32 rows, tiles of BN keys
 template <typename T, int DP, int NW, int BN, bool CAP, bool BIAS>
-__global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : 2) void k_attn_fwd(const AtFwd a)
+__global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 ? 4 : 2) void k_attn_fwd(const AtFwd a)
 {
     typedef AtNum<T> Num;
     typedef AtTile<NW * 64, BN, DP> Tile;
