@@ -518,31 +518,31 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
         for (int i = 0; i < 16; ++i) dk[d][i] = dv[d][i] = 0.0f;
 
     const uint32_t plain_at = at_address(lds) + at_plain_lane<DP>(lane), trans_at = at_address(lds) + at_trans_lane<DP>(lane);
-    auto work = [&](int at, const uint32_t *in, bool whole) __attribute__((always_inline)) {
-        const uint32_t qa = plain_at + at, ga = qa + kTile, qt = trans_at + at, gt = qt + kTile;
-        // A wave issues in order, and at 128 elements it is alone on its SIMD: what is to run beside a product has to stand between
-        // products, and what a product reads has to be on its way well before.  Fences keep the order below: scores; do.v with the
-        // exponentials between its products and dv's operands read meanwhile; dv with ds between; dk.
-        constexpr int kPer = 16 / kKs;               // scores per product
-        at_acc x, y;
-        float slope[CAP ? 16 : 1];
-        u32x4 fq[kKs], fg[kKs], p[2], ds[2];
-        auto row4 = [&](int word, int w) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4 *>(in + word * 32 + 8 * w + 4 * half); };   // rows of registers 4w..4w+3
-#pragma unroll
-        for (int ks = 0; ks < kKs; ++ks) fq[ks] = at_plain<DP>(qa, 0, ks);
-#pragma unroll
-        for (int ks = 0; ks < kKs; ++ks) fg[ks] = at_plain<DP>(ga, 0, ks);
-        u32x4 l4[4], d4[4], sl4[BIAS ? 4 : 1], pl4[BIAS ? 4 : 1];
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            d4[w] = row4(kAbDelta, w);
-            l4[w] = row4(kAbLse, w);
+    // A wave issues in order, and at 128 elements it is alone on its SIMD: what is to run beside a product has to stand between
+    // products, and what a product reads has to be on its way well before.  Fences keep the order below: scores; do.v with the
+    // exponentials between its products and dv's operands read meanwhile; dv with ds between; dk, with the next tile's rows read.
+    constexpr int kPer = 16 / kKs;                   // scores per product
+    u32x4 fq[kKs], fg[kKs], l4[4], d4[4], sl4[BIAS ? 4 : 1], pl4[BIAS ? 4 : 1];
+    auto read = [&](int at, const uint32_t *in, int ks) __attribute__((always_inline)) {      // a part of the rows and of what is known of them
+        fq[ks] = at_plain<DP>(plain_at + at, 0, ks);
+        fg[ks] = at_plain<DP>(plain_at + at + kTile, 0, ks);
+        if (ks < 4) {
+            const uint32_t *q = in + 8 * ks + 4 * half;                // rows of registers 4ks..4ks+3
+            l4[ks] = *reinterpret_cast<const u32x4 *>(q + kAbLse * 32);
+            d4[ks] = *reinterpret_cast<const u32x4 *>(q + kAbDelta * 32);
             if (BIAS) {
-                sl4[w] = row4(kAbSlope, w);
-                pl4[w] = row4(kAbPlace, w);
+                sl4[ks] = *reinterpret_cast<const u32x4 *>(q + kAbSlope * 32);
+                pl4[ks] = *reinterpret_cast<const u32x4 *>(q + kAbPlace * 32);
             }
         }
-        __builtin_amdgcn_sched_barrier(0);
+    };
+    static_assert(kKs >= 4, "four parts of what is known of the rows");
+    // at_next: the tile to read meanwhile, if any
+    auto work = [&](int at, const uint32_t *in, bool whole, bool more, int at_next, const uint32_t *in_next) __attribute__((always_inline)) {
+        const uint32_t qt = trans_at + at, gt = qt + kTile;
+        at_acc x, y;
+        float slope[CAP ? 16 : 1];
+        u32x4 p[2], ds[2];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             x[i] = 0.0f;
@@ -572,7 +572,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
         if (!whole) {
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                const u32x4 lo4 = row4(kAbLo, w), hi4 = row4(kAbHi, w);
+                const u32x4 lo4 = *reinterpret_cast<const u32x4 *>(in + kAbLo * 32 + 8 * w + 4 * half), hi4 = *reinterpret_cast<const u32x4 *>(in + kAbHi * 32 + 8 * w + 4 * half);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     const bool vis = uint32_t(j_own - int(lo4[c])) < hi4[c] - lo4[c];
@@ -601,12 +601,17 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
-        for (int n = 0; n < kKs; ++n) dk[n % kDt] = Num::mfma(fg[n], ds[n / kDt], dk[n % kDt]);
+        for (int n = 0; n < kKs; ++n) {
+            dk[n % kDt] = Num::mfma(fg[n], ds[n / kDt], dk[n % kDt]);
+            if (more) read(at_next, in_next, n);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
     int t = __builtin_amdgcn_readfirstlane(next());
     if (t >= 0) fetch(t);
     for (int cur = 0; t >= 0; cur ^= 1) {
         char *p = lds + cur * 4 * kTile;
+        const int at = cur * 4 * kTile;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -618,11 +623,15 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
         info[cur][tid >> 7][tid & 127] = word;
         if (BIAS && tid < 128) info[cur][tid >> 6][(128 + (tid & 63)) % (kInfo * 32)] = word2;
         __syncthreads();
+        const int u0 = t & 1 ? 0 : 1;                // the first of the two tiles that this wave's keys meet (the other one is read for nothing where there is none)
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) read(at + u0 * 2 * kTile, info[cur][u0], ks);
+        __builtin_amdgcn_sched_barrier(0);
         const int after = __builtin_amdgcn_readfirstlane(next());
         if (after >= 0) fetch(after);
-#pragma unroll 1
-        for (int u = 0; u < 2; ++u)
-            if (t >> u & 1) work(cur * 4 * kTile + u * 2 * kTile, info[cur][u], t >> (2 + u) & 1);
+        __builtin_amdgcn_sched_barrier(0);
+        if (t & 1) work(at, info[cur][0], t >> 2 & 1, true, at + 2 * kTile, info[cur][1]);
+        if (t & 2) work(at + 2 * kTile, info[cur][1], t >> 3 & 1, false, 0, nullptr);
         t = after;
     }
     if (j_own >= s.Nk) return;
