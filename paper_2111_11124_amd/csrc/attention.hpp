@@ -115,20 +115,22 @@ __device__ __forceinline__ int at_place(const AtShape &s, int b, uint32_t token)
 // linear in the row's bits: turn(a ^ b) = turn(a) ^ turn(b)
 template <int DP> __device__ __forceinline__ constexpr int at_turn(int row) { return ((row & 3) << 1) ^ ((row >> 2) & (DP == 128 ? 1 : 7)); }
 
-// ROWS x DP elements from memory to LDS by NT threads, by way of registers.  Rows past `rows` and pieces past D become zeros.
-// `at(row)`: byte offset of a row from `base`.
+// ROWS x DP elements from memory to LDS by NT threads, by way of registers.  Rows past `rows` and pieces past D become zeros: they lie
+// outside of the span, whose end is the last row's (rows that overlap in memory, as where one key stands for all, come again instead).
 template <int NT, int ROWS, int DP> struct AtTile {
     static constexpr int kPieces = DP / 8, kN = ROWS * kPieces / NT, kBytes = ROWS * DP * 2;
-    static_assert(ROWS * kPieces % NT == 0, "whole pieces per thread");
+    static_assert(ROWS * kPieces % NT == 0 && NT % kPieces == 0, "whole rows per step of the threads");
     u32x4 r[kN];
-    template <typename At> __device__ __forceinline__ void load(const char *base, int rows, int D, At at)
+    __device__ static __forceinline__ uint32_t place(uint32_t stride, int D)       // of this thread's first piece
     {
-        const Span s(base, kNowhere);
+        const int piece = int(threadIdx.x) % kPieces;
+        return piece * 8 < D ? uint32_t(int(threadIdx.x) / kPieces) * stride + piece * 16 : kNowhere;
+    }
+    __device__ __forceinline__ void load(const char *base, int rows, uint32_t stride, int D, uint32_t at)
+    {
+        const Span s(base, uint32_t((rows < ROWS ? rows : ROWS) - 1) * stride + uint32_t(D) * 2);
 #pragma unroll
-        for (int k = 0; k < kN; ++k) {
-            const int i = int(threadIdx.x) + k * NT, row = i / kPieces, piece = i % kPieces;
-            s.load_kept(row < rows && piece * 8 < D ? uint32_t(at(row)) + piece * 16 : kNowhere, r[k]);
-        }
+        for (int k = 0; k < kN; ++k) s.load_kept(at == kNowhere ? kNowhere : at + uint32_t(k * (NT / kPieces)) * stride, r[k]);
     }
     __device__ __forceinline__ void keep(uint64_t rows)      // rows without a bit become zeros
     {

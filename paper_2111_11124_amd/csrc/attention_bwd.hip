@@ -31,7 +31,7 @@ struct AbOrder {
 enum { kAbLse = 0, kAbDelta, kAbLo, kAbHi, kAbSlope, kAbPlace, kAbEmpty, kAbWords };   // 32 words of each per tile
 struct AbRows {                        // what the row pass leaves
     uint32_t *info;                    // [b * Hk + key head][tile][word][place]: log-sum-exp in powers of two (3e38 where nothing is seen), -delta,
-                                       // interval, slope in powers of two, place of the query, 1 where nothing is seen
+                                       // interval, slope in powers of two, place of the query, 1.0f where nothing is seen
     int4 *tiles;                       // [..][tile]: least lo, largest hi of the rows that see something; largest lo, least hi of all
     float2 *most;                      // [..][four tiles]: largest |do|, largest |delta|   (binary16 only)
     float *values;                     // [..][128 keys]: largest |v|                       (binary16 only)
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(kThreads) void k_attn_rows(const AtBwd a)
                 p[kAbHi * 32] = uint32_t(hi);
                 p[kAbSlope * 32] = __float_as_uint(slope2);
                 p[kAbPlace * 32] = uint32_t(place);
-                p[kAbEmpty * 32] = hi == 0;
+                p[kAbEmpty * 32] = __float_as_uint(hi == 0 ? 1.0f : 0.0f);
                 if (x == 0) a.w.tiles[at] = make_int4(l0, h1, l1, h0);
             }
             if (x == 0) empty[tid >> 5] = uint32_t(none >> (tid & 32));
@@ -291,10 +291,14 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
 
     const char *kbase = a.k.p + int64_t(b) * a.k.batch + int64_t(hk) * a.k.head, *vbase = a.v.p + int64_t(b) * a.v.batch + int64_t(hk) * a.v.head;
     Tile tk, tv;
-    auto fetch = [&](int t) __attribute__((always_inline)) {
-        const int j0 = t * BN;
-        tk.load(kbase + int64_t(j0) * a.k.token, s.Nk - j0, s.D, [&](int x) { return x * int(a.k.token); });
-        tv.load(vbase + int64_t(j0) * a.v.token, s.Nk - j0, s.D, [&](int x) { return x * int(a.v.token); });
+    const uint32_t k_step = uint32_t(a.k.token), v_step = uint32_t(a.v.token), k_at = Tile::place(k_step, s.D), v_at = Tile::place(v_step, s.D);
+    kbase += int64_t(t0) * BN * a.k.token;
+    vbase += int64_t(t0) * BN * a.v.token;
+    auto fetch = [&](int t) __attribute__((always_inline)) {        // t0, t0 + 1, ...
+        tk.load(kbase, s.Nk - t * BN, k_step, s.D, k_at);
+        tv.load(vbase, s.Nk - t * BN, v_step, s.D, v_at);
+        kbase += int64_t(BN) * a.k.token;
+        vbase += int64_t(BN) * a.v.token;
     };
     at_acc dq[kDt];
 #pragma unroll
@@ -444,26 +448,25 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
     const uint32_t *words = a.w.info + int64_t(head) * order.tiles * (kAbWords * 32);
     const int pairs = int(order.tiles / 2), mine = (pairs - int(split) + int(a.splits) - 1) / int(a.splits);   // this workgroup's: split, split + splits, ...
 
-    // this thread's pieces of a tile: the rows' places within it
-    uint32_t q_at[kOff], g_at[kOff], lds_at[kOff], empty_at[kOff];
-    int dt[kOff], dg[kOff];
+    // this thread's pieces of a tile: the rows' places within it.  A tile is cut short by the tokens that are left or, where a token's
+    // heads are more than a tile, by the heads: `cut` counts what the cut goes by.
+    const bool long_tokens = order.parts > 1;
+    uint32_t q_at[kOff], g_at[kOff], lds_at[kOff];
+    int cut[kOff];
     const int piece = tid % kPieces;
 #pragma unroll
     for (int k = 0; k < kOff; ++k) {
-        const int x = tid / kPieces + k * (256 / kPieces);
-        dt[k] = int(fastdiv(uint32_t(x), order.div_heads));
-        dg[k] = x - dt[k] * order.heads;
-        const bool in = dt[k] < order.tokens && piece * 8 < s.D;
-        q_at[k] = uint32_t(dt[k]) * uint32_t(a.q.token) + uint32_t(dg[k]) * uint32_t(a.q.head) + piece * 16;
-        g_at[k] = uint32_t(dt[k]) * uint32_t(a.dO.token) + uint32_t(dg[k]) * uint32_t(a.dO.head) + piece * 16;
+        const int x = tid / kPieces + k * (256 / kPieces), dt = int(fastdiv(uint32_t(x), order.div_heads)), dg = x - dt * order.heads;
+        q_at[k] = uint32_t(dt) * uint32_t(a.q.token) + uint32_t(dg) * uint32_t(a.q.head) + piece * 16;
+        g_at[k] = uint32_t(dt) * uint32_t(a.dO.token) + uint32_t(dg) * uint32_t(a.dO.head) + piece * 16;
         lds_at[k] = x * (DP * 2) + ((piece ^ at_turn<DP>(x)) << 4);
-        empty_at[k] = (kAbEmpty * 32 + x) * 4;
-        if (!in) dt[k] = 0x40000000;
+        cut[k] = dt < order.tokens && piece * 8 < s.D ? (long_tokens ? dg : dt) : 0x40000000;
     }
 
-    // the next pair of tiles that this workgroup's keys meet: 64 summaries at a time, one per lane; what each wave makes of them
-    int base = -64;
-    uint64_t meets = 0, mine0 = 0, mine1 = 0, whole0 = 0, whole1 = 0, some = 0;
+    // the next pair of tiles that this workgroup's keys meet: 64 summaries at a time, one per lane, and what this wave makes of them
+    enum { kMine = 1, kWhole = 4, kSome = 16 };       // (twice) the wave's keys are met; are seen by all rows; some row sees nothing
+    int base = -64, flags = 0;
+    uint64_t meets = 0;
     auto next = [&]() __attribute__((always_inline)) {
         while (meets == 0) {
             base += 64;
@@ -475,41 +478,52 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
                 t[0] = p[0];
                 t[1] = p[1];
             }
-            meets = __ballot((t[0].y > k0 && t[0].x < k0 + kAbKeys) || (t[1].y > k0 && t[1].x < k0 + kAbKeys));
-            mine0 = __ballot(t[0].y > j0 && t[0].x < j0 + 32);
-            mine1 = __ballot(t[1].y > j0 && t[1].x < j0 + 32);
-            whole0 = __ballot(t[0].w >= j0 + 32 && t[0].z <= j0);
-            whole1 = __ballot(t[1].w >= j0 + 32 && t[1].z <= j0);
-            some = __ballot(t[0].w == 0 || t[1].w == 0);
+            bool in = false;
+            flags = 0;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                in |= t[u].y > k0 && t[u].x < k0 + kAbKeys;
+                if (t[u].y > j0 && t[u].x < j0 + 32) flags |= kMine << u;
+                if (t[u].w >= j0 + 32 && t[u].z <= j0) flags |= kWhole << u;
+                if (t[u].w == 0) flags |= kSome;
+            }
+            meets = __ballot(in);
         }
         const int bit = __builtin_ctzll(meets);
         meets &= meets - 1;
-        return ((int(split) + (base + bit) * int(a.splits)) << 5) | int(mine0 >> bit & 1u) | int(mine1 >> bit & 1u) << 1 | int(whole0 >> bit & 1u) << 2 | int(whole1 >> bit & 1u) << 3 |
-               int(some >> bit & 1u) << 4;
+        return ((int(split) + (base + bit) * int(a.splits)) << 5) | __builtin_amdgcn_readlane(flags, bit);
     };
     u32x4 tq[2][kOff], tg[2][kOff];
-    uint32_t dead[2][kOff], word, word2 = 0;
+    uint32_t word, word2 = 0;
+    const int64_t q_tile = int64_t(order.tokens) * a.q.token, g_tile = int64_t(order.tokens) * a.dO.token;
+    const uint32_t word_at = (tid >> 7) * (kAbWords * 128) + (tid & 127) * 4, word2_at = ((tid >> 6) & 1) * (kAbWords * 128) + (128 + (tid & 63)) * 4;
     auto fetch = [&](int what) __attribute__((always_inline)) {
-        const bool check = what & 16;                  // some row of these tiles sees nothing
         const uint32_t pair = uint32_t(what >> 5);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const uint32_t tile = pair * 2 + u, t = order.parts == 1 ? tile : fastdiv(tile, order.div_parts);
-            const int64_t token = int64_t(t) * order.tokens;
-            const int g0 = int(tile - t * order.parts) * 32, left = int(s.Nq - token < 64 ? s.Nq - token : 64), heads = s.G - g0;
-            const Span q(qbase + token * a.q.token + int64_t(g0) * a.q.head, kNowhere), g(gbase + token * a.dO.token + int64_t(g0) * a.dO.head, kNowhere);
-            const Span e(words + int64_t(tile) * (kAbWords * 32), check ? kAbWords * 128 : 0);
+            const uint32_t tile = pair * 2 + u;
+            const char *qp = qbase, *gp = gbase;
+            int left;
+            if (!long_tokens) {
+                qp += int64_t(tile) * q_tile;
+                gp += int64_t(tile) * g_tile;
+                left = s.Nq - int(tile) * order.tokens;
+            } else {
+                const uint32_t t = fastdiv(tile, order.div_parts), g0 = (tile - t * uint32_t(order.parts)) * 32;
+                qp += int64_t(t) * a.q.token + int64_t(g0) * a.q.head;
+                gp += int64_t(t) * a.dO.token + int64_t(g0) * a.dO.head;
+                left = int(t) < s.Nq ? s.G - int(g0) : 0;
+            }
+            const Span q(qp, kNowhere), g(gp, kNowhere);
 #pragma unroll
             for (int k = 0; k < kOff; ++k) {
-                const bool in = dt[k] < left && dg[k] < heads;
-                q.load_kept(in ? q_at[k] : kNowhere, tq[u][k]);
-                g.load_kept(in ? g_at[k] : kNowhere, tg[u][k]);
-                dead[u][k] = __float_as_uint(e.load_f32(empty_at[k]));   // zero where nothing is to be checked
+                q.load_kept(cut[k] < left ? q_at[k] : kNowhere, tq[u][k]);
+                g.load_kept(cut[k] < left ? g_at[k] : kNowhere, tg[u][k]);
             }
         }
-        const uint32_t *p = words + int64_t(pair) * 2 * (kAbWords * 32);
-        word = p[(tid >> 7) * (kAbWords * 32) + (tid & 127)];
-        if (BIAS) word2 = p[((tid >> 6) & 1) * (kAbWords * 32) + 128 + (tid & 63)];
+        const Span p(words + int64_t(pair) * 2 * (kAbWords * 32), 2 * kAbWords * 128);
+        word = __float_as_uint(p.load_f32(word_at));
+        if (BIAS) word2 = __float_as_uint(p.load_f32(word2_at));
     };
     at_acc dk[kDt], dv[kDt];
 #pragma unroll
@@ -612,13 +626,20 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
     for (int cur = 0; t >= 0; cur ^= 1) {
         char *p = lds + cur * 4 * kTile;
         const int at = cur * 4 * kTile;
+        if (t & kSome) {
+            const Span e(words + int64_t(t >> 5) * 2 * (kAbWords * 32), 2 * kAbWords * 128);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int k = 0; k < kOff; ++k)
+                    if (e.load_f32(((u * kAbWords + kAbEmpty) * 32 + tid / kPieces + k * (256 / kPieces)) * 4) != 0.0f) tq[u][k] = tg[u][k] = u32x4{0u, 0u, 0u, 0u};
+        }
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int k = 0; k < kOff; ++k) {
-                const u32x4 keep = dead[u][k] ? u32x4{0u, 0u, 0u, 0u} : u32x4{~0u, ~0u, ~0u, ~0u};
-                *reinterpret_cast<u32x4 *>(p + u * 2 * kTile + lds_at[k]) = tq[u][k] & keep;
-                *reinterpret_cast<u32x4 *>(p + u * 2 * kTile + kTile + lds_at[k]) = tg[u][k] & keep;
+                *reinterpret_cast<u32x4 *>(p + u * 2 * kTile + lds_at[k]) = tq[u][k];
+                *reinterpret_cast<u32x4 *>(p + u * 2 * kTile + kTile + lds_at[k]) = tg[u][k];
             }
         info[cur][tid >> 7][tid & 127] = word;
         if (BIAS && tid < 128) info[cur][tid >> 6][(128 + (tid & 63)) % (kInfo * 32)] = word2;

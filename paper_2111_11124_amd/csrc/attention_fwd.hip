@@ -209,10 +209,14 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 ? 4 : 2) void k_att
 
     const char *kbase = a.k.p + int64_t(b) * a.k.batch + int64_t(hk) * a.k.head, *vbase = a.v.p + int64_t(b) * a.v.batch + int64_t(hk) * a.v.head;
     Tile tk, tv;
-    auto fetch = [&](int t) __attribute__((always_inline)) {
-        const int j0 = t * BN;
-        tk.load(kbase + int64_t(j0) * a.k.token, s.Nk - j0, s.D, [&](int x) { return x * int(a.k.token); });
-        tv.load(vbase + int64_t(j0) * a.v.token, s.Nk - j0, s.D, [&](int x) { return x * int(a.v.token); });
+    const uint32_t k_step = uint32_t(a.k.token), v_step = uint32_t(a.v.token), k_at = Tile::place(k_step, s.D), v_at = Tile::place(v_step, s.D);
+    kbase += int64_t(t0) * BN * a.k.token;
+    vbase += int64_t(t0) * BN * a.v.token;
+    auto fetch = [&](int t) __attribute__((always_inline)) {        // t0, t0 + 1, ...
+        tk.load(kbase, s.Nk - t * BN, k_step, s.D, k_at);
+        tv.load(vbase, s.Nk - t * BN, v_step, s.D, v_at);
+        kbase += int64_t(BN) * a.k.token;
+        vbase += int64_t(BN) * a.v.token;
     };
 
     at_acc o[kDt];
