@@ -28,10 +28,15 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hi
          f"-I{INCLUDE}", f"-I{CSRC}"]
 
 
+# Matrix-core sums in ordinary registers: a kernel with more than 256 of them otherwise moves each score between the two register
+# files before and after it is worked on, one instruction each way.
+MORE_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for src in ("attention_fwd.hip", "attention_bwd.hip")}
+
+
 def _compile(src: str) -> Path:
     OBJ.mkdir(exist_ok=True)
     out = OBJ / (src + ".o")
-    cmd = [HIPCC, *FLAGS, "-c", str(CSRC / src), "-o", str(out)]
+    cmd = [HIPCC, *FLAGS, *MORE_FLAGS.get(src, []), "-c", str(CSRC / src), "-o", str(out)]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         sys.stderr.write(r.stdout + r.stderr)
