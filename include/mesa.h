@@ -467,7 +467,7 @@ mesa_status mesa_attention_bounds(int32_t *lo, int32_t *hi, int64_t B, int64_t N
  * sequence sees, and rows of q, o and do whose query sees nothing, does not matter (infinities and NaN neither).
  * Storage is binary16 or bfloat16; scores, softmax and sums are binary32, the probabilities that enter a product are rounded to dt.
  * 1 <= Hk, Hq a multiple of Hk; D a multiple of 8, 8 <= D <= 128, else MESA_ERR_UNSUPPORTED (MESA_F32 too).
- * Nq, Nk < 2^30, Nq * (Hq/Hk) < 2^31; scale > 0 and cap >= 0, finite.  Nk = 0: o = 0, lse = -infinity.
+ * Nq, Nk < 2^30, Nq * (Hq/Hk) < 2^31, Nq * D and Nk * D < 2^34, and what a launch can have of workgroups; scale > 0 and cap >= 0, finite.  Nk = 0: o = 0, lse = -infinity.
  */
 typedef struct mesa_attention {
     int64_t B, Nq, Nk, Hq, Hk, D;

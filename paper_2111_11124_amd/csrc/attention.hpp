@@ -258,7 +258,9 @@ inline mesa_status at_supported(const mesa_attention &a, mesa_dtype dt)
 {
     if (!valid_dtype(dt) || !at_valid(a)) return MESA_ERR_INVALID_ARG;
     if (dt == MESA_F32 || a.D % 8 != 0 || a.D > 128) return MESA_ERR_UNSUPPORTED;
-    if (a.Nq * (a.Hq / a.Hk) >= (int64_t(1) << 31)) return MESA_ERR_UNSUPPORTED;
+    // rows and pieces of a head are counted in 32 bits, workgroups by what a launch takes; below these, products of two sizes fit 64 bits
+    const int64_t top = int64_t(1) << 31;
+    if (a.Nq >= top / (a.Hq / a.Hk) || a.Nq >= top * 8 / a.D || a.Nk >= top * 8 / a.D || a.B > most_workgroups(256) / a.Hk) return MESA_ERR_UNSUPPORTED;
     return MESA_OK;
 }
 AtShape at_shape(const mesa_attention &a, const mesa_attention_mask &m);

@@ -67,26 +67,38 @@ struct AtBwd {
     uint32_t heads, key_blocks, splits, row_blocks;
 };
 
-// codes to contiguous (B, heads, tokens, D) elements, as mesa_dequantize; eight per thread
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_attn_operand(AtView q, const float *__restrict__ alpha, const float *__restrict__ beta, char *__restrict__ out, int heads, int tokens,
-                                                           int D, int64_t pieces)
+// codes to contiguous (B, heads, tokens, D) elements, as mesa_dequantize; eight per thread, up to three operands in one launch
+struct AbCodes {
+    AtView q;
+    const float *alpha, *beta;
+    char *out;
+    int32_t heads, tokens;
+    uint32_t first, per_head;          // workgroups: the operand's first one, those of a (sequence, head)
+};
+struct AbOperands {
+    AbCodes c[3];
+    int32_t count, D;
+    FastDiv div_d;                     // by D / 8
+};
+template <typename T> __global__ __launch_bounds__(kThreads) void k_attn_operand(const AbOperands a)
 {
-    const int64_t id = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-    if (id >= pieces) return;
-    const int per = D / 8;
-    const int64_t row = id / per, bh = row / tokens, b = bh / heads;
-    const int e = int(id - row * per) * 8, t = int(row - bh * tokens), h = int(bh - b * heads);
-    const u32x2 c = *reinterpret_cast<const u32x2 *>(q.p + b * q.batch + int64_t(t) * q.token + int64_t(h) * q.head + e);
+    int n = 0;
+    if (a.count > 1 && blockIdx.x >= a.c[1].first) n = 1;
+    if (a.count > 2 && blockIdx.x >= a.c[2].first) n = 2;
+    const AbCodes &c = n == 0 ? a.c[0] : n == 1 ? a.c[1] : a.c[2];
+    const uint32_t blk = blockIdx.x - c.first, bh = blk / c.per_head, b = bh / uint32_t(c.heads), h = bh - b * uint32_t(c.heads);
+    const uint32_t i = (blk - bh * c.per_head) * kThreads + threadIdx.x, t = fastdiv(i, a.div_d), e = (i - t * uint32_t(a.D / 8)) * 8;
+    if (t >= uint32_t(c.tokens)) return;
+    const u32x2 v = *reinterpret_cast<const u32x2 *>(c.q.p + int64_t(b) * c.q.batch + int64_t(t) * c.q.token + int64_t(h) * c.q.head + e);
     float f[8];
-    codes_to_float(c, f);
-    const float s = alpha[h] / 255.0f, z = beta[h];
+    codes_to_float(v, f);
+    const float s = c.alpha[h] / 255.0f, z = c.beta[h];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
         const float y = f[k] * s;
         f[k] = y + z;
     }
-    Store<T>::store(out, row * D + e, Store<T>::pack(f));
+    Store<T>::store(c.out, (int64_t(bh) * c.tokens + t) * a.D + e, Store<T>::pack(f));
 }
 
 // The row pass.  Workgroups [0, blocks) of a head: the deltas of 128 places, log-sum-exps, intervals and the summaries of their four
@@ -417,32 +429,6 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
             vf[ks] = at_column(v, ks, lane, s.D);
         }
     }
-    float mul = 1.0f, undo = s.scale, undo_v = 1.0f;
-    if (Num::kHalf) {
-        float ss = 0.0f, most = 0.0f, most_delta = 0.0f;
-#pragma unroll
-        for (int ks = 0; ks < kKs; ++ks) {
-            float f[8];
-            Store<T>::unpack(vf[ks], f);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) ss = fmaf(f[k], f[k], ss);
-        }
-        ss = at_pair_sum(ss);
-        for (uint32_t k = lane; k < a.w.blocks; k += 64) {
-            const float2 m = a.w.most[int64_t(head) * a.w.blocks + k];
-            most = fmaxf(most, m.x);
-            most_delta = fmaxf(most_delta, m.y);
-        }
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            most = fmaxf(most, __shfl_xor(most, m, 64));
-            most_delta = fmaxf(most_delta, __shfl_xor(most_delta, m, 64));
-        }
-        const int e = ab_exponent(sqrtf(ss) * most + most_delta);
-        mul = ab_pow2(e - kAtDrop);
-        undo = s.scale * ab_pow2(-e);
-        undo_v = ab_pow2(-kAtDrop);
-    }
     const char *qbase = a.q.p + int64_t(b) * a.q.batch + int64_t(hk) * s.G * a.q.head, *gbase = a.dO.p + int64_t(b) * a.dO.batch + int64_t(hk) * s.G * a.dO.head;
     const int4 *tiles = a.w.tiles + int64_t(head) * order.tiles;
     const uint32_t *words = a.w.info + int64_t(head) * order.tiles * (kAbWords * 32);
@@ -532,6 +518,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
         for (int i = 0; i < 16; ++i) dk[d][i] = dv[d][i] = 0.0f;
 
     const uint32_t plain_at = at_address(lds) + at_plain_lane<DP>(lane), trans_at = at_address(lds) + at_trans_lane<DP>(lane);
+    float mul = 1.0f, undo = s.scale, undo_v = 1.0f;
     // A wave issues in order, and at 128 elements it is alone on its SIMD: what is to run beside a product has to stand between
     // products, and what a product reads has to be on its way well before.  Fences keep the order below: scores; do.v with the
     // exponentials between its products and dv's operands read meanwhile; dv with ds between; dk, with the next tile's rows read.
@@ -622,7 +609,32 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
         }
     };
     int t = __builtin_amdgcn_readfirstlane(next());
-    if (t >= 0) fetch(t);
+    if (t >= 0) fetch(t);                            // on its way while the factors below are formed
+    if (Num::kHalf) {
+        float ss = 0.0f, most = 0.0f, most_delta = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks) {
+            float f[8];
+            Store<T>::unpack(vf[ks], f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) ss = fmaf(f[k], f[k], ss);
+        }
+        ss = at_pair_sum(ss);
+        for (uint32_t k = lane; k < a.w.blocks; k += 64) {
+            const float2 m = a.w.most[int64_t(head) * a.w.blocks + k];
+            most = fmaxf(most, m.x);
+            most_delta = fmaxf(most_delta, m.y);
+        }
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            most = fmaxf(most, __shfl_xor(most, m, 64));
+            most_delta = fmaxf(most_delta, __shfl_xor(most_delta, m, 64));
+        }
+        const int e = ab_exponent(sqrtf(ss) * most + most_delta);
+        mul = ab_pow2(e - kAtDrop);
+        undo = s.scale * ab_pow2(-e);
+        undo_v = ab_pow2(-kAtDrop);
+    }
     for (int cur = 0; t >= 0; cur ^= 1) {
         char *p = lds + cur * 4 * kTile;
         const int at = cur * 4 * kTile;
@@ -800,15 +812,29 @@ static mesa_status at_bwd(const mesa_attention &m, AtBwd &a, const AtBwdPlan &p,
     AtView *view[3] = {&a.q, &a.k, &a.v};
     const int64_t tokens[3] = {m.Nq, m.Nk, m.Nk}, heads[3] = {m.Hq, m.Hk, m.Hk};
     char *out = ws + p.info + p.part;
+    AbOperands ops;
+    ops.count = 0;
+    ops.D = int32_t(m.D);
+    ops.div_d = make_fastdiv(uint32_t(m.D / 8));
+    int64_t blocks = 0;
     for (int k = 0; k < 3; ++k) {
         if (!codes[k]) continue;
-        const int64_t pieces = m.B * tokens[k] * heads[k] * (m.D / 8);
-        const AtView c = {static_cast<const char *>(in[k].data), in[k].batch, in[k].token, in[k].head};
-        hipLaunchKernelGGL(k_attn_operand<T>, dim3(uint32_t(ceil_div(pieces, kThreads))), dim3(kThreads), 0, s, c, in[k].alpha, in[k].beta, out, int(heads[k]), int(tokens[k]),
-                           int(m.D), pieces);
-        if (const mesa_status st = launch_status()) return st;
+        AbCodes &c = ops.c[ops.count++];
+        c.q = AtView{static_cast<const char *>(in[k].data), in[k].batch, in[k].token, in[k].head};
+        c.alpha = in[k].alpha;
+        c.beta = in[k].beta;
+        c.out = out;
+        c.heads = int32_t(heads[k]);
+        c.tokens = int32_t(tokens[k]);
+        c.first = uint32_t(blocks);
+        c.per_head = uint32_t(ceil_div(tokens[k] * (m.D / 8), kThreads));
+        blocks += m.B * heads[k] * int64_t(c.per_head);
         *view[k] = AtView{out, heads[k] * tokens[k] * m.D * 2, m.D * 2, tokens[k] * m.D * 2};
         out += p.operand[k];
+    }
+    if (ops.count) {
+        hipLaunchKernelGGL(k_attn_operand<T>, dim3(uint32_t(blocks)), dim3(kThreads), 0, s, ops);
+        if (const mesa_status st = launch_status()) return st;
     }
     return m.D <= 64 ? at_bwd_forms<T, 64>(a, m.cap > 0.0f, bias, s) : at_bwd_forms<T, 128>(a, m.cap > 0.0f, bias, s);
 }
@@ -848,8 +874,10 @@ extern "C" MESA_EXPORT mesa_status mesa_attention_bwd_q(mesa_attention a, mesa_a
         !at_strides(a, a.Nq, group, dq.batch, dq.token, dq.head) || !at_strides(a, a.Nk, 1, dk.batch, dk.token, dk.head) || !at_strides(a, a.Nk, 1, dv.batch, dv.token, dv.head))
         return MESA_ERR_INVALID_ARG;
     const AtBwdPlan p = at_bwd_plan(a, codes);
-    const int64_t heads = a.B * a.Hk, most = most_workgroups(256), quads = (a.Nq > a.Nk ? a.Nq * group : a.Nk * (group > 2 ? group : 2)) * (a.D / 4);
-    if (heads * p.key_blocks * p.splits > most || heads * (int64_t(p.blocks) + p.key_blocks) > most || heads * quads > most * kThreads) return MESA_ERR_UNSUPPORTED;
+    const int64_t heads = a.B * a.Hk, most = most_workgroups(256), rows = heads * a.Nq * group, keys = heads * a.Nk, operands = (rows + 2 * keys) * (a.D / 8) / kThreads + heads * (group + 2);
+    if (heads * p.key_blocks * p.splits > most || heads * (int64_t(p.blocks) + p.key_blocks) > most || heads * p.row_blocks > most || operands > most ||
+        (rows > 2 * keys ? rows : 2 * keys) * (a.D / 4) > most * kThreads)
+        return MESA_ERR_UNSUPPORTED;
     if (a.Nq > 0 && a.Nk > 0 && (!ws || !aligned16(ws) || ws_bytes < p.total)) return MESA_ERR_WORKSPACE;
     AtBwd f;
     f.s = at_shape(a, m);

@@ -82,6 +82,9 @@ def test_attention_refusals(L):
     for kw in (dict(D=60), dict(D=136), dict(D=256)):
         assert attend(L, shape(**kw)) == no and attend_bwd(L, shape(**kw)) == no, kw
         assert m.attention_bwd_q_workspace_bytes(shape(**kw)) == 0
+    for kw in (dict(Nq=1 << 29, D=128), dict(Nk=1 << 28, D=64), dict(Nq=1 << 28, Hq=32), dict(B=1 << 24), dict(B=1 << 29, Hq=1 << 29, Hk=1 << 29)):
+        assert attend(L, shape(**kw)) == no and attend_bwd(L, shape(**kw)) == no, kw
+        assert m.attention_bwd_q_workspace_bytes(shape(**kw)) == 0 and m.attention_fwd_workspace_bytes(shape(**kw)) == 0
     a = shape()
     assert attend(L, a, dt=m.F32) == no and attend_bwd(L, a, dt=m.F32) == no and attend(L, a, dt=7) == bad
     wrong = (dict(data=P + 8), dict(data=None), dict(token=252), dict(head=60), dict(batch=4), dict(token=-8), dict(token=1 << 23), dict(head=1 << 30))
