@@ -46,6 +46,11 @@ template <> struct AtNum<_Float16> {
         p.y = _Float16(b);
         return as_u32(p);
     }
+    __device__ static __forceinline__ uint32_t rest(float a, float b, uint32_t w)      // what pack left of them
+    {
+        const h2 p = as_h2(w);
+        return pack(a - float(p.x), b - float(p.y));
+    }
 };
 template <> struct AtNum<__bf16> {
     static constexpr bool kHalf = false;
@@ -60,6 +65,7 @@ template <> struct AtNum<__bf16> {
         p.y = __bf16(b);
         return __builtin_bit_cast(uint32_t, p);
     }
+    __device__ static __forceinline__ uint32_t rest(float a, float b, uint32_t w) { return pack(a - __uint_as_float(w << 16), b - __uint_as_float(w & 0xFFFF0000u)); }
 };
 
 // a tensor (B, tokens, heads, D) as the kernels see it; strides in bytes
@@ -212,8 +218,15 @@ __device__ __forceinline__ int at_wave_max(int v)
 
 __device__ __forceinline__ float at_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// tanh of x, for u = 2 log2(e) x:  1 - 2 / (2^u + 1); off by some 1e-7 in absolute value, as is the score by 1e-7 caps
-__device__ __forceinline__ float at_tanh(float u) { return fmaf(-2.0f, __builtin_amdgcn_rcpf(at_exp2(u) + 1.0f), 1.0f); }
+// tanh of x, for u = 2 log2(e) x.  EXACT:  (2^u - 1) / (2^u + 1) -- the difference is exact where it is small, so that what is left of an error is
+// that of 2^u; times the cap it is a score's, which the forward hands on in lse (from 2^80 on the quotient is one).  Else  1 - 2 / (2^u + 1), two
+// instructions less and off by twice that, 1e-7: for the backward, whose probabilities are rounded to 16 bits.
+template <bool EXACT> __device__ __forceinline__ float at_tanh(float u)
+{
+    if (!EXACT) return fmaf(-2.0f, __builtin_amdgcn_rcpf(at_exp2(u) + 1.0f), 1.0f);
+    const float e = at_exp2(fminf(u, 80.0f));
+    return (e - 1.0f) * __builtin_amdgcn_rcpf(e + 1.0f);
+}
 
 // index within a 32-row accumulator tile of register i, without the lane's part 4*(lane/32)
 __device__ __forceinline__ constexpr int at_reg_row(int i) { return 8 * (i / 4) + i % 4; }

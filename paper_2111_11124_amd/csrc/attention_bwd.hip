@@ -226,7 +226,7 @@ __device__ __forceinline__ float ab_pow2(int e) { return __uint_as_float(uint32_
 template <bool CAP> __device__ __forceinline__ float ab_score(const AtShape &s, float x, float &slope)
 {
     if (!CAP) return x * s.c;
-    const float t = at_tanh(x * s.c);
+    const float t = at_tanh<false>(x * s.c);
     slope = fmaf(-t, t, 1.0f);
     return s.cap2 * t;
 }
@@ -234,7 +234,7 @@ template <bool CAP> __device__ __forceinline__ float ab_score(const AtShape &s, 
 // ---------------------------------------------------------------------------------------------
 // dq: a wave owns 32 rows
 // ---------------------------------------------------------------------------------------------
-template <typename T, int DP, int NW, int BN, bool CAP, bool BIAS>
+template <typename T, int DP, int NW, int BN, bool CAP, bool BIAS, bool FINE>
 __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
 {
     typedef AtNum<T> Num;
@@ -363,7 +363,14 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
             for (int g = 0; g < 2; ++g)
 #pragma unroll
                 for (int d = 0; d < kDt; ++d) {
-                    dq[d] = Num::mfma(at_transposed<DP>(kt, t * 32 + g * 16, d * 32), ds[g], dq[d]);
+                    const u32x4 f = at_transposed<DP>(kt, t * 32 + g * 16, d * 32);
+                    dq[d] = Num::mfma(f, ds[g], dq[d]);
+                    if (FINE) {
+                        u32x4 rest;
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) rest[w] = Num::rest(x[8 * g + 2 * w], x[8 * g + 2 * w + 1], ds[g][w]);
+                        dq[d] = Num::mfma(f, rest, dq[d]);
+                    }
                     if (d == kDt - 1) __builtin_amdgcn_sched_barrier(0);
                 }
         }
@@ -403,7 +410,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
 // ---------------------------------------------------------------------------------------------
 // A step is two tiles of 32 rows.  Where a tile lies at the edge of what its rows see, probabilities are set to zero element by
 // element; rows that see nothing are zeros in LDS, so that what they hold does not enter.
-template <typename T, int DP, bool CAP, bool BIAS>
+template <typename T, int DP, bool CAP, bool BIAS, bool FINE>
 __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd a)
 {
     typedef AtNum<T> Num;
@@ -543,7 +550,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
         const uint32_t qt = trans_at + at, gt = qt + kTile;
         at_acc x, y;
         float slope[CAP ? 16 : 1];
-        u32x4 p[2], ds[2];
+        u32x4 p[2], ds[2], p_rest[2], ds_rest[2];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             x[i] = 0.0f;
@@ -585,11 +592,15 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
-            for (int w = 0; w < 4; ++w) p[g][w] = Num::pack(x[8 * g + 2 * w], x[8 * g + 2 * w + 1]);
+            for (int w = 0; w < 4; ++w) {
+                p[g][w] = Num::pack(x[8 * g + 2 * w], x[8 * g + 2 * w + 1]);
+                if (FINE) p_rest[g][w] = Num::rest(x[8 * g + 2 * w], x[8 * g + 2 * w + 1], p[g][w]);
+            }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int n = 0; n < kKs; ++n) {
             dv[n % kDt] = Num::mfma(fq[n], p[n / kDt], dv[n % kDt]);
+            if (FINE) dv[n % kDt] = Num::mfma(fq[n], p_rest[n / kDt], dv[n % kDt]);
             fg[n] = at_transposed<DP>(qt, n / kDt * 16, n % kDt * 32);        // dk's operands
 #pragma unroll
             for (int i = n * kPer; i < n * kPer + kPer; ++i) {
@@ -598,12 +609,16 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
                 if (Num::kHalf) y[i] *= mul;
             }
 #pragma unroll
-            for (int w = n * kPer / 2; w < (n + 1) * kPer / 2; ++w) ds[w / 4][w % 4] = Num::pack(y[2 * w], y[2 * w + 1]);
+            for (int w = n * kPer / 2; w < (n + 1) * kPer / 2; ++w) {
+                ds[w / 4][w % 4] = Num::pack(y[2 * w], y[2 * w + 1]);
+                if (FINE) ds_rest[w / 4][w % 4] = Num::rest(y[2 * w], y[2 * w + 1], ds[w / 4][w % 4]);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int n = 0; n < kKs; ++n) {
             dk[n % kDt] = Num::mfma(fg[n], ds[n / kDt], dk[n % kDt]);
+            if (FINE) dk[n % kDt] = Num::mfma(fg[n], ds_rest[n / kDt], dk[n % kDt]);
             if (more) read(at_next, in_next, n);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -772,26 +787,33 @@ static AtBwdPlan at_bwd_plan(const mesa_attention &a, const bool codes[3])
     return p;
 }
 
-template <typename T, int DP, bool CAP, bool BIAS> static mesa_status at_bwd_launch(const AtBwd &a, hipStream_t s)
+template <typename T, int DP, bool CAP, bool BIAS, bool FINE> static mesa_status at_bwd_launch(const AtBwd &a, hipStream_t s)
 {
-    hipLaunchKernelGGL((k_attn_dkv<T, DP, CAP, BIAS>), dim3(a.heads * a.key_blocks * a.splits), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_attn_dkv<T, DP, CAP, BIAS, FINE>), dim3(a.heads * a.key_blocks * a.splits), dim3(256), 0, s, a);
     if (const mesa_status st = launch_status()) return st;
     if (a.splits > 1) {
         const int64_t pieces = int64_t(a.heads) * a.s.Nk * (a.s.D / 2);
         hipLaunchKernelGGL(k_attn_add<T>, dim3(uint32_t(ceil_div(pieces, kThreads))), dim3(kThreads), 0, s, a, pieces);
         if (const mesa_status st = launch_status()) return st;
     }
-    hipLaunchKernelGGL((k_attn_dq<T, DP, 4, 32, CAP, BIAS>), dim3(a.heads * a.row_blocks), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_attn_dq<T, DP, 4, 32, CAP, BIAS, FINE>), dim3(a.heads * a.row_blocks), dim3(256), 0, s, a);
     return launch_status();
+}
+// Up to kAbFine keys the call is bound by what it reads and writes (14 products of 64 keys to a row's four vectors), and with so few terms to
+// a sum the products' roundings do not average out: there probabilities and score gradients enter in two 16-bit parts.
+constexpr int kAbFine = 64;
+template <typename T, int DP, bool CAP, bool BIAS> static mesa_status at_bwd_parts(const AtBwd &a, hipStream_t s)
+{
+    return a.s.Nk <= kAbFine ? at_bwd_launch<T, DP, CAP, BIAS, true>(a, s) : at_bwd_launch<T, DP, CAP, BIAS, false>(a, s);
 }
 template <typename T, int DP> static mesa_status at_bwd_forms(const AtBwd &a, bool cap, bool bias, hipStream_t s)
 {
     hipLaunchKernelGGL((k_attn_rows<T, DP>), dim3(a.heads * (a.w.blocks + (AtNum<T>::kHalf ? a.w.key_blocks : 0))), dim3(kThreads), 0, s, a);
     if (const mesa_status st = launch_status()) return st;
-    if (cap && bias) return at_bwd_launch<T, DP, true, true>(a, s);
-    if (cap) return at_bwd_launch<T, DP, true, false>(a, s);
-    if (bias) return at_bwd_launch<T, DP, false, true>(a, s);
-    return at_bwd_launch<T, DP, false, false>(a, s);
+    if (cap && bias) return at_bwd_parts<T, DP, true, true>(a, s);
+    if (cap) return at_bwd_parts<T, DP, true, false>(a, s);
+    if (bias) return at_bwd_parts<T, DP, false, true>(a, s);
+    return at_bwd_parts<T, DP, false, false>(a, s);
 }
 template <typename T> static mesa_status at_zero(const AtOut &o, int64_t B, int64_t tokens, int64_t heads, int64_t D, hipStream_t s)
 {

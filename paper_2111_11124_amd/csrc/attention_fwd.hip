@@ -154,7 +154,7 @@ struct AtFwd {
 
 // NW waves of 32 rows, tiles of BN keys
 template <typename T, int DP, int NW, int BN, bool CAP, bool BIAS>
-__global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 ? 4 : 2) void k_attn_fwd(const AtFwd a)
+__global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 && !BIAS ? 4 : 2) void k_attn_fwd(const AtFwd a)
 {
     typedef AtNum<T> Num;
     typedef AtTile<NW * 64, BN, DP> Tile;
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 ? 4 : 2) void k_att
             for (int t = 0; t < kSub; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    if (CAP) x[t][i] = s.cap2 * at_tanh(x[t][i] * s.c);
+                    if (CAP) x[t][i] = s.cap2 * at_tanh<true>(x[t][i] * s.c);
                     else x[t][i] *= s.c;
                     if (BIAS) x[t][i] = fmaf(-slope2, fabsf(away - float(t * 32 + at_reg_row(i))), x[t][i]);
                 }
