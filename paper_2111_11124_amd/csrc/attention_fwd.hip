@@ -189,6 +189,7 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 && !BIAS ? 4 : 2) v
     }
     const float slope2 = BIAS ? s.slopes[hq] * kLog2e : 0.0f;
     const int place = BIAS ? at_place(s, b, row.token) : 0;
+    const float to_score = CAP ? s.cap2 : s.c;      // to powers of two, from tanh or from the product
     __syncthreads();
     int blo = 0x7FFFFFFF, bhi = 0, full_lo[NW], full_hi[NW];      // the same of the workgroup's rows; what each wave's rows see, all of them
 #pragma unroll
@@ -247,9 +248,8 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 && !BIAS ? 4 : 2) v
             for (int t = 0; t < kSub; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    if (CAP) x[t][i] = s.cap2 * at_tanh<true>(x[t][i] * s.c);
-                    else x[t][i] *= s.c;
-                    if (BIAS) x[t][i] = fmaf(-slope2, fabsf(away - float(t * 32 + at_reg_row(i))), x[t][i]);
+                    if (CAP) x[t][i] = at_tanh<true>(x[t][i] * s.c);
+                    if (BIAS) x[t][i] = fmaf(x[t][i], to_score, -slope2 * fabsf(away - float(t * 32 + at_reg_row(i))));
                 }
         }
         if (!whole) {
@@ -264,8 +264,8 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 && !BIAS ? 4 : 2) v
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, x[t][i]);
         top = at_pair_max(top);
-        constexpr bool kRaw = !CAP && !BIAS;       // the factor c is then still to come (c > 0)
-        if (kRaw) top *= s.c;
+        constexpr bool kRaw = !BIAS;               // the factor is then still to come (it is positive)
+        if (kRaw) top *= to_score;
         // the sums are scaled anew only where a row's maximum has grown by more than 2^8: probabilities up to 2^8 are as exact
         if (__ballot(top > m + 8.0f)) {
             const float m1 = fmaxf(m, top), f = at_exp2(m - m1);
@@ -285,7 +285,7 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 && !BIAS ? 4 : 2) v
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const int i = 8 * g + 2 * w;
-                    const float e0 = at_exp2(kRaw ? fmaf(x[t][i], s.c, -m) : x[t][i] - m), e1 = at_exp2(kRaw ? fmaf(x[t][i + 1], s.c, -m) : x[t][i + 1] - m);
+                    const float e0 = at_exp2(kRaw ? fmaf(x[t][i], to_score, -m) : x[t][i] - m), e1 = at_exp2(kRaw ? fmaf(x[t][i + 1], to_score, -m) : x[t][i + 1] - m);
                     l += e0;
                     l1 += e1;
                     p[2 * t + g][w] = Num::pack(e0, e1);

@@ -105,6 +105,11 @@ CASES = [  # B, Nq, Nk, Hq, Hk, D, mask, cap, bias, layout
     (3, 90, 33, 2, 2, 64, dict(causal=True), 0, False, "bnhd"),          # queries before the first key see nothing
     (2, 40, 100, 4, 2, 128, dict(causal=True, docs=5, pad=True, start=(-20, 90)), 0, True, "bnhd"),
     (1, 1000, 1000, 1, 1, 64, {}, 0, False, "bnhd"),
+    # more heads to a key head than a tile has rows, and not a multiple of it; widths that end within a piece of either tile
+    (1, 70, 70, 40, 1, 64, dict(causal=True), 0, False, "bnhd"),
+    (2, 21, 37, 66, 2, 24, dict(causal=True, docs=3), 10.0, True, "bnhd"),
+    (1, 130, 130, 33, 1, 120, dict(window=20, pad=True), 0, False, "bnhd"),
+    (1, 200, 200, 5, 1, 72, {}, 0, False, "packed"),
 ]
 FEW = [  # few rows over many keys: the keys are shared out
     (1, 1, 5000, 8, 1, 128, dict(causal=True), 0, False, "bnhd"),
