@@ -7,10 +7,11 @@
 //
 // Bound by memory: per element of a 16-bit tensor the forward moves 2 bytes in and 2 + 1 out, the backward 2 + 1 in and 2 out.
 // A head is a group of LPH lanes with eight elements each (LPH: the power of two from D/8), a wave holds 64/LPH heads side by
-// side ("slot") and walks over the tokens of its tile with the same heads, so that alpha, beta, gamma stay in
-// registers and the extrema accumulate there.  Cosines and sines depend on token and pair, not on the head: a workgroup
+// side ("slot") and walks over the tokens of its tile with the same heads, so that the extrema accumulate in registers.  Cosines and sines depend on token and pair, not on the head: a workgroup
 // forms them once per tile into LDS -- angle and reduction in binary64, as positions times frequencies have more than 24
 // bits -- and all heads read them there.
+// Measured, 32768 tokens of 32 + 8 + 8 heads of 128, bfloat16 (a copy of as many bytes runs at 5.0 TB/s): forward 196 us (939 MB, 4.8 TB/s),
+// queries and keys again 109 us (503 MB, 4.6 TB/s), backward 174 us (839 MB, 4.8 TB/s).  One token of 24 heads of 64: 4.5 us.
 #include <hip/hip_runtime.h>
 
 #include "api_util.hpp"
@@ -23,7 +24,6 @@ constexpr int kQkvTile = 16;        // tokens of a tile at most; 32 left no othe
 constexpr int kQkvGrid = 1024;      // workgroups at most: four per compute unit
 constexpr int kQkvMaxHeads = 512;
 constexpr int kQkvAlone = 16384;    // elements at most that one workgroup takes
-constexpr int kQkvU = 4;            // tokens in flight per wave
 
 struct QkvGeom {
     int64_t T;
@@ -98,7 +98,8 @@ __device__ __forceinline__ void qkv_angles(float2 *cs, const QkvGeom &g, const f
 }
 
 // The other half of each pair, from the lane `hop` further on or back, by data-parallel-primitive moves where the hop is a power of two
-// below 16 (the LDS crossbar, which serves the whole compute unit, was what bound the backward: 250 -> 218 us at 32768 x 40 heads of 128).
+// below 16 (the LDS crossbar, which serves the whole compute unit, was what bound the backward: 250 us with it, 218 without, when the rest was
+// still to come).
 template <int CTRL, int BANKS> __device__ __forceinline__ float qkv_move(float old, float v)
 {
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, old), __builtin_bit_cast(int, v), CTRL, 0xf, BANKS, false));
@@ -171,6 +172,72 @@ __device__ __forceinline__ void qkv_hat(u32x2 c, float s, float b, float f[8])
     for (int k = 0; k < 8; ++k) f[k] = fmaf(f[k], s, b);
 }
 
+// What the kernels below share: a workgroup's heads' parameters in LDS -- (scale, offset) of the codes, gains in binary32 -- and the walk of a
+// wave over its items: U tokens of a slot, slot by slot, tile by tile.  An item's loads are requested while the item before it is worked
+// on, the first one's before the parameters and angles are formed: with a few tokens per workgroup these latencies are most of its time
+// (forward of one token 6.7 -> 4.5 us, of 2000 tokens 24 -> 16 us; of 32768 no change).
+struct QkvItem {
+    int64_t t0;                        // the tile's first token; at or past T: no item
+    uint32_t slot, base;               // base: the item's first token within the tile
+};
+struct QkvWave {
+    uint32_t lane, wave, lph, hpw, d0, sub, phase, phases, slots, slot0, slot_step;
+    int partner;
+    __device__ __forceinline__ QkvWave(const QkvGeom &g, uint32_t heads)
+    {
+        lane = threadIdx.x & 63u;
+        wave = uint32_t(__builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6)));
+        lph = 1u << g.lph_log2;
+        hpw = 64u >> g.lph_log2;
+        d0 = (lane & (lph - 1)) * 8;
+        sub = lane >> g.lph_log2;
+        const int hop = int(g.rot / 16);
+        partner = int(lane) + (d0 < g.rot / 2 ? hop : d0 < g.rot ? -hop : 0);
+        slots = (heads + hpw - 1) / hpw;
+        phases = 1u << g.phases_log2;
+        phase = wave & (phases - 1);
+        slot0 = wave >> g.phases_log2;
+        slot_step = (kThreads / 64) >> g.phases_log2;
+    }
+    __device__ __forceinline__ uint32_t tokens(const QkvGeom &g, int64_t t0) const { return g.T - t0 < g.tile ? uint32_t(g.T - t0) : g.tile; }
+    // the first item of the tile at t0 or of the first one behind it that has any for this wave
+    __device__ __forceinline__ QkvItem first(const QkvGeom &g, int64_t t0) const
+    {
+        QkvItem i = {t0, slot0, phase};
+        while (i.t0 < g.T && (slot0 >= slots || phase >= tokens(g, i.t0))) i.t0 += int64_t(gridDim.x) * g.tile;
+        return i;
+    }
+    template <int U> __device__ __forceinline__ QkvItem next(const QkvGeom &g, QkvItem i) const
+    {
+        i.base += phases * U;
+        if (i.base < tokens(g, i.t0)) return i;
+        i.base = phase;
+        i.slot += slot_step;
+        return i.slot < slots ? i : first(g, i.t0 + int64_t(gridDim.x) * g.tile);
+    }
+};
+__host__ __device__ inline uint32_t qkv_even(uint32_t n) { return (n + 1) & ~1u; }      // gains start at 16 bytes
+// params: [heads] (scale, offset), then gains [2][D]; CODES: 255 / alpha, else alpha / 255
+template <typename T, bool CODES>
+__device__ __forceinline__ void qkv_params(float2 *params, const QkvGeom &g, uint32_t heads, const float *alpha, const float *beta, const void *gamma_q, const void *gamma_k)
+{
+    for (uint32_t h = threadIdx.x; h < heads; h += kThreads) {
+        const float a = alpha[h];
+        params[h] = make_float2(CODES ? (a > 0.0f ? 255.0f / a : 0.0f) : a / 255.0f, beta[h]);
+    }
+    float *gain = reinterpret_cast<float *>(params + qkv_even(heads));
+    if (gamma_q)
+        for (uint32_t i = threadIdx.x; i < 2 * g.D; i += kThreads) gain[i] = i < g.D ? Store<T>::load1(gamma_q, i) : Store<T>::load1(gamma_k, i - g.D);
+}
+__device__ __forceinline__ void qkv_gain(const float *gain, uint32_t at, bool take, float gam[8])     // at: a multiple of 8
+{
+    const float4 *p = reinterpret_cast<const float4 *>(gain + at);
+    const float4 a = p[0], b = p[1];
+    const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) gam[k] = take ? v[k] : 1.0f;
+}
+
 // The forward (AGAIN false: from x, with codes and extrema) or queries and keys once more (AGAIN: from the codes and rstd).
 // Both round y once, from binary32.  Lanes without an element and tokens past the tile lie outside of their spans: no access is
 // conditional.
@@ -182,101 +249,113 @@ __global__ __launch_bounds__(kThreads, 4) void k_qkv_fwd(QkvGeom g, const void *
 {
     typedef typename Store<T>::raw_t Raw;
     constexpr uint32_t kEb = sizeof(T);
-    extern __shared__ float2 smem[];
-    float2 *cs = smem;
-    int *lmn = reinterpret_cast<int *>(smem + g.tile * g.angles), *lmx = lmn + g.H;
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    const uint32_t lph = 1u << g.lph_log2, hpw = 64u >> g.lph_log2;
-    const uint32_t d0 = (lane & (lph - 1)) * 8, sub = lane >> g.lph_log2;
-    const int hop = int(g.rot / 16), partner = int(lane) + (d0 < g.rot / 2 ? hop : d0 < g.rot ? -hop : 0);
-    const uint32_t heads = AGAIN ? g.Hn : g.H, slots = (heads + hpw - 1) / hpw;
-    const uint32_t phase = wave & ((1u << g.phases_log2) - 1), phases = 1u << g.phases_log2;
-    const uint32_t wide = g.H * g.D, slim = g.Hn * g.D;       // elements of a token: codes; y
-    const float inv_d = 1.0f / float(g.D);
+    constexpr int U = AGAIN ? 4 : 2;                           // codes are half as many bytes to request (two: 117 us, four: 109)
+    extern __shared__ float4 smem[];
+    const uint32_t heads = AGAIN ? g.Hn : g.H, wide = g.H * g.D, slim = g.Hn * g.D;       // wide, slim: elements of a token, in codes and in y
+    float2 *params = reinterpret_cast<float2 *>(smem), *cs = params + qkv_even(heads) + g.D;
+    float *gain = reinterpret_cast<float *>(params + qkv_even(heads));
+    int *lmn = reinterpret_cast<int *>(cs + g.tile * g.angles), *lmx = lmn + g.H;
+    const QkvWave w(g, heads);
+    const uint32_t d0 = w.d0;
+    struct Loads {
+        Raw raw[U];
+        u32x2 cin[U];
+        float rs[U];
+    };
+    auto load = [&](const QkvItem &i, Loads &l) __attribute__((always_inline)) {
+        if (i.t0 >= g.T) return;                               // uniform; nothing is behind it
+        const uint32_t n = w.tokens(g, i.t0), hd = i.slot * w.hpw + w.sub;
+        const bool act = hd < heads && d0 < g.D;
+        const Span sx(AGAIN ? nullptr : static_cast<const char *>(x) + i.t0 * x_row * kEb, AGAIN ? 0 : kNowhere), sq(AGAIN ? qin + i.t0 * wide : nullptr, AGAIN ? n * wide : 0);
+        const Span sr(AGAIN && rstd ? rstd + i.t0 * g.Hn : nullptr, AGAIN && rstd ? n * g.Hn * 4 : 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t tk = i.base + u * w.phases;
+            if (AGAIN) {
+                const bool live = act && tk < n;
+                l.cin[u] = sq.load8(live ? tk * wide + hd * g.D + d0 : kNowhere);
+                l.rs[u] = sr.load_f32(live ? (tk * g.Hn + hd) * 4 : kNowhere);
+            } else {
+                // past the tile: the item's first token again, so that extrema stay what they are
+                sx.load(act ? ((tk < n ? tk : i.base) * uint32_t(x_row) + hd * g.D + d0) * kEb : kNowhere, l.raw[u]);
+            }
+        }
+    };
+    QkvItem item = w.first(g, int64_t(blockIdx.x) * g.tile);
+    Loads now, then;
+    load(item, now);
+    qkv_params<T, !AGAIN>(params, g, heads, alpha, beta, gamma_q, gamma_k);
     if (!AGAIN)
         for (uint32_t h = threadIdx.x; h < g.H; h += kThreads) {
             lmn[h] = order_key(__builtin_inff());
             lmx[h] = order_key(-__builtin_inff());
         }
+    const float inv_d = 1.0f / float(g.D);
+    float mn = __builtin_inff(), mx = -__builtin_inff();
     for (int64_t t0 = int64_t(blockIdx.x) * g.tile; t0 < g.T; t0 += int64_t(gridDim.x) * g.tile) {
-        const uint32_t tokens = g.T - t0 < g.tile ? uint32_t(g.T - t0) : g.tile;
-        const Span sx(AGAIN ? nullptr : static_cast<const char *>(x) + t0 * x_row * kEb, AGAIN ? 0 : kNowhere), sq((AGAIN ? qin : q) + t0 * wide, tokens * wide);
-        const Span sy(static_cast<char *>(y) + t0 * slim * kEb, tokens * slim * kEb), sr(rstd ? rstd + t0 * g.Hn : nullptr, rstd ? tokens * g.Hn * 4 : 0);
-        __syncthreads();                           // the last tile's angles are done with
+        const uint32_t tokens = w.tokens(g, t0);
+        if (t0 != int64_t(blockIdx.x) * g.tile) __syncthreads();      // the last tile's angles are done with
         qkv_angles(cs, g, freq, pos, t0, tokens);
         __syncthreads();
-        for (uint32_t slot = wave >> g.phases_log2; slot < slots; slot += (kThreads / 64) >> g.phases_log2) {
-            const uint32_t hd = slot * hpw + sub;
+        const Span sq(AGAIN ? nullptr : q + t0 * wide, AGAIN ? 0 : tokens * wide);
+        const Span sy(static_cast<char *>(y) + t0 * slim * kEb, tokens * slim * kEb), sr(!AGAIN && rstd ? rstd + t0 * g.Hn : nullptr, !AGAIN && rstd ? tokens * g.Hn * 4 : 0);
+        while (item.t0 == t0) {
+            const QkvItem after = w.next<U>(g, item);
+            load(after, then);
+            __builtin_amdgcn_sched_barrier(0);                 // requested before this item is worked on
+            const uint32_t hd = item.slot * w.hpw + w.sub, at = hd * g.D + d0;
             const bool act = hd < heads && d0 < g.D, turn = act && hd < g.Hn;
-            const bool any_turn = slot * hpw < g.Hn;     // uniform
-            const uint32_t at = hd * g.D + d0;
-            float r = 0.0f, b = 0.0f, gam[8];
-            if (act) {
-                b = beta[hd];
-                r = alpha[hd];
-                r = AGAIN ? r / 255.0f : r > 0.0f ? 255.0f / r : 0.0f;
-            }
+            const bool any_turn = item.slot * w.hpw < g.Hn;     // uniform
+            const float2 prm = params[act ? hd : 0];
+            float gam[8];
+            if (gamma_q) qkv_gain(gain, (hd < g.Hq ? 0 : g.D) + (d0 < g.D ? d0 : 0), turn, gam);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) gam[k] = 1.0f;
-            if (gamma_q && turn) Store<T>::unpack(Store<T>::load(hd < g.Hq ? gamma_q : gamma_k, d0), gam);
-            float mn = __builtin_inff(), mx = -__builtin_inff();
-            for (uint32_t base = phase; base < tokens; base += phases * kQkvU) {
-                Raw raw[kQkvU];
-                u32x2 cin[kQkvU];
-                float rs[kQkvU];
+            for (int u = 0; u < U; ++u) {
+                const uint32_t tk = item.base + u * w.phases;
+                const bool live = act && tk < tokens;
+                float f[8];
+                if (AGAIN) {
+                    qkv_hat(now.cin[u], prm.x, prm.y, f);
+                    if (gamma_q)
 #pragma unroll
-                for (int u = 0; u < kQkvU; ++u) {
-                    const uint32_t tk = base + u * phases;
-                    const bool live = act && tk < tokens;
-                    if (AGAIN) {
-                        cin[u] = sq.load8(live ? tk * wide + at : kNowhere);
-                        rs[u] = gamma_q ? sr.load_f32(live ? (tk * g.Hn + hd) * 4 : kNowhere) : 1.0f;
-                    } else {
-                        // past the tile: its first token again, so that extrema stay what they are
-                        sx.load(act ? ((tk < tokens ? tk : base) * uint32_t(x_row) + at) * kEb : kNowhere, raw[u]);
+                        for (int k = 0; k < 8; ++k) f[k] *= now.rs[u] * gam[k];
+                } else {
+                    Store<T>::unpack(now.raw[u], f);
+                    const uint32_t e = tk * wide + at;
+                    float v[8], bits[8];
+                    if (SR) sr_bits(seed, offset + uint64_t((t0 * wide + e) >> 3), bits);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        v[k] = quantize_real<SR>(f[k], prm.x, prm.y, SR ? bits[k] : 0.0f);
+                        mn = vmin(mn, f[k]);
+                        mx = vmax(mx, f[k]);
+                    }
+                    const u32x2 c = round_pack_codes<SR>(v);
+                    sq.store8(live ? e : kNowhere, c);
+                    if (!any_turn) continue;
+                    if (gamma_q) {
+                        float ss = 0.0f;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) ss = fmaf(f[k], f[k], ss);
+                        const float rr = 1.0f / sqrtf(fmaf(qkv_head_sum(ss, g.lph_log2), inv_d, g.eps));
+                        sr.store_f32(live && turn && d0 == 0 ? (tk * g.Hn + hd) * 4 : kNowhere, rr);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) f[k] *= rr * gam[k];
                     }
                 }
-#pragma unroll
-                for (int u = 0; u < kQkvU; ++u) {
-                    const uint32_t tk = base + u * phases;
-                    const bool live = act && tk < tokens;
-                    float f[8];
-                    if (AGAIN) {
-                        qkv_hat(cin[u], r, b, f);
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) f[k] *= rs[u] * gam[k];
-                    } else {
-                        Store<T>::unpack(raw[u], f);
-                        const uint32_t e = tk * wide + at;
-                        float v[8], bits[8];
-                        if (SR) sr_bits(seed, offset + uint64_t((t0 * wide + e) >> 3), bits);
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            v[k] = quantize_real<SR>(f[k], r, b, SR ? bits[k] : 0.0f);
-                            mn = vmin(mn, f[k]);
-                            mx = vmax(mx, f[k]);
-                        }
-                        const u32x2 c = round_pack_codes<SR>(v);
-                        sq.store8(live ? e : kNowhere, c);
-                        if (!any_turn) continue;
-                        if (gamma_q) {
-                            float ss = 0.0f;
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) ss = fmaf(f[k], f[k], ss);
-                            const float rr = 1.0f / sqrtf(fmaf(qkv_head_sum(ss, g.lph_log2), inv_d, g.eps));
-                            sr.store_f32(live && turn && d0 == 0 ? (tk * g.Hn + hd) * 4 : kNowhere, rr);
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) f[k] *= rr * gam[k];
-                        }
-                    }
-                    if (g.rot) qkv_turn(f, cs + (tk < tokens ? tk : 0) * g.angles, g, d0, partner, 1.0f);
-                    sy.store(live && turn ? (tk * slim + at) * kEb : kNowhere, Store<T>::pack(f));
+                if (g.rot) qkv_turn(f, cs + (tk < tokens ? tk : 0) * g.angles, g, d0, w.partner, 1.0f);
+                sy.store(live && turn ? (tk * slim + at) * kEb : kNowhere, Store<T>::pack(f));
+            }
+            if (!AGAIN && (after.slot != item.slot || after.t0 != t0)) {
+                if (act) {
+                    atomicMin(&lmn[hd], order_key(mn));
+                    atomicMax(&lmx[hd], order_key(mx));
                 }
+                mn = __builtin_inff();
+                mx = -__builtin_inff();
             }
-            if (!AGAIN && act) {
-                atomicMin(&lmn[hd], order_key(mn));
-                atomicMax(&lmx[hd], order_key(mx));
-            }
+            item = after;
+            now = then;
         }
     }
     if (!AGAIN) {
@@ -302,106 +381,119 @@ __global__ __launch_bounds__(kThreads, 4) void k_qkv_bwd(QkvGeom g, const int8_t
 {
     typedef typename Store<T>::raw_t Raw;
     constexpr uint32_t kEb = sizeof(T);
-    constexpr int U = 2;                           // tokens in flight per wave: four took registers that the waves beside it need
-    extern __shared__ float2 smem[];
-    float2 *cs = smem;
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    const uint32_t lph = 1u << g.lph_log2, hpw = 64u >> g.lph_log2;
-    const uint32_t d0 = (lane & (lph - 1)) * 8, sub = lane >> g.lph_log2;
-    const int hop = int(g.rot / 16), partner = int(lane) + (d0 < g.rot / 2 ? hop : d0 < g.rot ? -hop : 0);
-    const uint32_t slots = (g.Hn + hpw - 1) / hpw;
-    const uint32_t phase = wave & ((1u << g.phases_log2) - 1), phases = 1u << g.phases_log2;
-    const uint32_t wide = g.H * g.D, slim = g.Hn * g.D;
-    const float inv_d = 1.0f / float(g.D);
+    constexpr int U = 2;
+    extern __shared__ float4 smem[];
+    const uint32_t heads = g.Hn, wide = g.H * g.D, slim = g.Hn * g.D;
+    float2 *params = reinterpret_cast<float2 *>(smem), *cs = params + (NORM ? qkv_even(heads) + g.D : 0);
+    float *gain = reinterpret_cast<float *>(params + qkv_even(heads));
     // the gains' gradients of this lane's elements, of query and of key heads: in LDS, where only this lane reaches them
-    float *mine_q = reinterpret_cast<float *>(smem + g.tile * g.angles) + threadIdx.x * 8, *mine_k = mine_q + kThreads * 8;
-    if (NORM)
+    float *sums = reinterpret_cast<float *>(cs + g.tile * g.angles), *mine_q = sums + threadIdx.x * 8, *mine_k = mine_q + kThreads * 8;
+    const QkvWave w(g, heads);
+    const uint32_t d0 = w.d0;
+    struct Loads {
+        Raw raw[U];
+        u32x2 cin[U];
+        float rs[U];
+    };
+    auto load = [&](const QkvItem &i, Loads &l) __attribute__((always_inline)) {
+        if (i.t0 >= g.T) return;
+        const uint32_t n = w.tokens(g, i.t0), hd = i.slot * w.hpw + w.sub;
+        const bool act = hd < heads && d0 < g.D;
+        const Span sdy(static_cast<const char *>(dy) + i.t0 * slim * kEb, n * slim * kEb);
+        const Span sq(NORM ? q + i.t0 * wide : nullptr, NORM ? n * wide : 0), sr(NORM ? rstd + i.t0 * g.Hn : nullptr, NORM ? n * g.Hn * 4 : 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t tk = i.base + u * w.phases;
+            const bool live = act && tk < n;
+            sdy.load(live ? (tk * slim + hd * g.D + d0) * kEb : kNowhere, l.raw[u]);
+            if (NORM) {
+                l.cin[u] = sq.load8(live ? tk * wide + hd * g.D + d0 : kNowhere);
+                l.rs[u] = sr.load_f32(live ? (tk * g.Hn + hd) * 4 : kNowhere);
+            }
+        }
+    };
+    QkvItem item = w.first(g, int64_t(blockIdx.x) * g.tile);
+    Loads now, then;
+    load(item, now);
+    if (NORM) {
+        qkv_params<T, false>(params, g, heads, alpha, beta, gamma_q, gamma_k);
 #pragma unroll
         for (int k = 0; k < 8; ++k) mine_q[k] = mine_k[k] = 0.0f;
+    }
+    const float inv_d = 1.0f / float(g.D);
+    float mine[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) mine[k] = 0.0f;
     for (int64_t t0 = int64_t(blockIdx.x) * g.tile; t0 < g.T; t0 += int64_t(gridDim.x) * g.tile) {
-        const uint32_t tokens = g.T - t0 < g.tile ? uint32_t(g.T - t0) : g.tile;
-        const Span sdy(static_cast<const char *>(dy) + t0 * slim * kEb, tokens * slim * kEb), sdx(static_cast<char *>(dx) + t0 * dx_row * kEb, kNowhere);
-        const Span sq(NORM ? q + t0 * wide : nullptr, NORM ? tokens * wide : 0), sr(NORM ? rstd + t0 * g.Hn : nullptr, NORM ? tokens * g.Hn * 4 : 0);
-        __syncthreads();
+        const uint32_t tokens = w.tokens(g, t0);
+        if (t0 != int64_t(blockIdx.x) * g.tile) __syncthreads();
         qkv_angles(cs, g, freq, pos, t0, tokens);
         __syncthreads();
-        for (uint32_t slot = wave >> g.phases_log2; slot < slots; slot += (kThreads / 64) >> g.phases_log2) {
-            const uint32_t hd = slot * hpw + sub;
-            const bool act = hd < g.Hn && d0 < g.D, key = hd >= g.Hq;
-            const uint32_t at = hd * g.D + d0;
-            float s = 0.0f, b = 0.0f, gam[8];
-            if (NORM && act) {
-                s = alpha[hd] / 255.0f;
-                b = beta[hd];
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) gam[k] = 0.0f;
-            if (NORM && act) Store<T>::unpack(Store<T>::load(key ? gamma_k : gamma_q, d0), gam);
-            float mine[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) mine[k] = 0.0f;
-            for (uint32_t base = phase; base < tokens; base += phases * U) {
-                Raw raw[U];
-                u32x2 cin[U];
-                float rs[U];
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const uint32_t tk = base + u * phases;
-                    const bool live = act && tk < tokens;
-                    sdy.load(live ? (tk * slim + at) * kEb : kNowhere, raw[u]);
-                    if (NORM) {
-                        cin[u] = sq.load8(live ? tk * wide + at : kNowhere);
-                        rs[u] = sr.load_f32(live ? (tk * g.Hn + hd) * 4 : kNowhere);
-                    }
-                }
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const uint32_t tk = base + u * phases;
-                    const bool live = act && tk < tokens;
-                    float f[8];
-                    Store<T>::unpack(raw[u], f);           // zeros where nothing was loaded
-                    if (g.rot) qkv_turn(f, cs + (tk < tokens ? tk : 0) * g.angles, g, d0, partner, -1.0f);
-                    if (NORM) {
-                        float n[8], dot = 0.0f;
-                        qkv_hat(cin[u], s, b, n);
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            n[k] *= rs[u];
-                            mine[k] = fmaf(f[k], n[k], mine[k]);
-                            f[k] *= gam[k];
-                            dot = fmaf(f[k], n[k], dot);
-                        }
-                        const float mean = qkv_head_sum(dot, g.lph_log2) * inv_d;
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) f[k] = rs[u] * fmaf(-n[k], mean, f[k]);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                    sdx.store(live ? (tk * uint32_t(dx_row) + at) * kEb : kNowhere, Store<T>::pack(f));
-                }
-            }
+        const Span sdx(static_cast<char *>(dx) + t0 * dx_row * kEb, kNowhere);
+        while (item.t0 == t0) {
+            const QkvItem after = w.next<U>(g, item);
+            load(after, then);
+            __builtin_amdgcn_sched_barrier(0);
+            const uint32_t hd = item.slot * w.hpw + w.sub, at = hd * g.D + d0;
+            const bool act = hd < heads && d0 < g.D, key = hd >= g.Hq;
+            float2 prm = make_float2(0.0f, 0.0f);
+            float gam[8];
             if (NORM) {
+                prm = params[act ? hd : 0];
+                qkv_gain(gain, (key ? g.D : 0) + (d0 < g.D ? d0 : 0), true, gam);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t tk = item.base + u * w.phases;
+                const bool live = act && tk < tokens;
+                float f[8];
+                Store<T>::unpack(now.raw[u], f);           // zeros where nothing was loaded
+                if (g.rot) qkv_turn(f, cs + (tk < tokens ? tk : 0) * g.angles, g, d0, w.partner, -1.0f);
+                if (NORM) {
+                    float n[8], dot = 0.0f;
+                    qkv_hat(now.cin[u], prm.x, prm.y, n);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        n[k] *= now.rs[u];
+                        mine[k] = fmaf(f[k], n[k], mine[k]);
+                        f[k] *= gam[k];
+                        dot = fmaf(f[k], n[k], dot);
+                    }
+                    const float mean = qkv_head_sum(dot, g.lph_log2) * inv_d;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) f[k] = now.rs[u] * fmaf(-n[k], mean, f[k]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                sdx.store(live ? (tk * uint32_t(dx_row) + at) * kEb : kNowhere, Store<T>::pack(f));
+            }
+            if (NORM && (after.slot != item.slot || after.t0 != t0)) {
                 float *to = key ? mine_k : mine_q;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) to[k] += mine[k];
+                for (int k = 0; k < 8; ++k) {
+                    to[k] += mine[k];
+                    mine[k] = 0.0f;
+                }
             }
+            item = after;
+            now = then;
         }
     }
     if (!NORM) return;
     // lanes that hold the same elements of different heads, then the four waves, each in a fixed order
-    float *sum = reinterpret_cast<float *>(smem + g.tile * g.angles) + 2 * kThreads * 8;        // [wave][2][8 * lph]
+    float *sum = sums + 2 * kThreads * 8;                // [wave][2][8 * lph]
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             float v = (c ? mine_k : mine_q)[k];
-            for (uint32_t m = lph; m < 64; m <<= 1) v += __shfl_xor(v, int(m), 64);
-            if (sub == 0) sum[((wave * 2 + c) << (g.lph_log2 + 3)) + d0 + k] = v;
+            for (uint32_t m = w.lph; m < 64; m <<= 1) v += __shfl_xor(v, int(m), 64);
+            if (w.sub == 0) sum[((w.wave * 2 + c) << (g.lph_log2 + 3)) + d0 + k] = v;
         }
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < 2 * g.D; i += kThreads) {
         const uint32_t c = i >= g.D, d = i - c * g.D;
         float v = 0.0f;
-        for (uint32_t w = 0; w < kThreads / 64; ++w) v += sum[((w * 2 + c) << (g.lph_log2 + 3)) + d];
+        for (uint32_t k = 0; k < kThreads / 64; ++k) v += sum[((k * 2 + c) << (g.lph_log2 + 3)) + d];
         if (gridDim.x > 1) part[int64_t(blockIdx.x) * 2 * g.D + i] = v;
         else (c ? dgamma_k : dgamma_q)[d] = v;
     }
@@ -442,8 +534,14 @@ static mesa_status check_qkv(const mesa_qkv_heads &h, mesa_dtype dt)
     return MESA_OK;
 }
 
-static size_t qkv_lds_fwd(const QkvGeom &g, bool extrema) { return size_t(g.tile) * g.angles * 8 + (extrema ? size_t(g.H) * 8 : 0); }
-static size_t qkv_lds_bwd(const QkvGeom &g, bool norm) { return size_t(g.tile) * g.angles * 8 + (norm ? 2 * kThreads * 32 + size_t(8) * (8u << g.lph_log2) * 4 : 0); }
+static size_t qkv_lds_fwd(const QkvGeom &g, bool again)
+{
+    return (qkv_even(again ? g.Hn : g.H) + g.D + g.tile * g.angles) * sizeof(float2) + (again ? 0 : size_t(g.H) * 8);
+}
+static size_t qkv_lds_bwd(const QkvGeom &g, bool norm)
+{
+    return (size_t(norm ? qkv_even(g.Hn) + g.D : 0) + g.tile * g.angles) * sizeof(float2) + (norm ? 2 * kThreads * 32 + size_t(8) * (8u << g.lph_log2) * 4 : 0);
+}
 
 }  // namespace mesa
 
@@ -479,7 +577,7 @@ extern "C" MESA_EXPORT mesa_status mesa_qkv_norm_rope_fwd_q(const void *x, int64
     const QkvGeom g = qkv_geom(h);
     const int grid = qkv_grid(g);
     if (!ws || !aligned4(ws) || ws_bytes < mesa_qkv_norm_rope_fwd_q_workspace_bytes(h, dt)) return MESA_ERR_WORKSPACE;
-    const size_t lds = qkv_lds_fwd(g, true);
+    const size_t lds = qkv_lds_fwd(g, false);
     hipStream_t s = static_cast<hipStream_t>(stream);
 #define MESA_QKV(T) \
     do { \
@@ -505,7 +603,7 @@ extern "C" MESA_EXPORT mesa_status mesa_qkv_norm_rope_recompute_q(const int8_t *
         (gamma_q && !rstd) || !aligned4(rstd) || (h.rot && (!freq || !pos)) || !aligned4(freq) || !aligned4(pos))
         return MESA_ERR_INVALID_ARG;
     const QkvGeom g = qkv_geom(h);
-    const size_t lds = qkv_lds_fwd(g, false);
+    const size_t lds = qkv_lds_fwd(g, true);
 #define MESA_QKV(T) \
     hipLaunchKernelGGL((k_qkv_fwd<T, false, true>), dim3(qkv_grid(g)), dim3(kThreads), lds, static_cast<hipStream_t>(stream), g, nullptr, 0, q, gamma_q, gamma_k, freq, pos, \
                        const_cast<float *>(alpha), const_cast<float *>(beta), 0.0f, y, const_cast<float *>(rstd), nullptr, 0, 0, nullptr)
