@@ -218,14 +218,14 @@ __device__ __forceinline__ int at_wave_max(int v)
 
 __device__ __forceinline__ float at_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// tanh of x, for u = 2 log2(e) x.  EXACT:  (2^u - 1) / (2^u + 1) -- the difference is exact where it is small, so that what is left of an error is
-// that of 2^u; times the cap it is a score's, which the forward hands on in lse (from 2^80 on the quotient is one).  Else  1 - 2 / (2^u + 1), two
-// instructions less and off by twice that, 1e-7: for the backward, whose probabilities are rounded to 16 bits.
+// tanh of x, for u = 2 log2(e) x.  EXACT:  (1 - 2^-|u|) / (1 + 2^-|u|) with the sign of u -- the difference is exact where it is small, so that
+// what is left of an error is that of the power; times the cap it is a score's, which the forward hands on in lse.  Else  1 - 2 / (2^u + 1),
+// two instructions less and off by twice that, 1e-7: for the backward, whose probabilities are rounded to 16 bits.  Both hand NaN on.
 template <bool EXACT> __device__ __forceinline__ float at_tanh(float u)
 {
     if (!EXACT) return fmaf(-2.0f, __builtin_amdgcn_rcpf(at_exp2(u) + 1.0f), 1.0f);
-    const float e = at_exp2(fminf(u, 80.0f));
-    return (e - 1.0f) * __builtin_amdgcn_rcpf(e + 1.0f);
+    const float e = at_exp2(-fabsf(u));
+    return __builtin_copysignf((1.0f - e) * __builtin_amdgcn_rcpf(1.0f + e), u);
 }
 
 // index within a 32-row accumulator tile of register i, without the lane's part 4*(lane/32)

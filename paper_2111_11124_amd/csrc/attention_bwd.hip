@@ -186,8 +186,9 @@ __global__ __launch_bounds__(kThreads) void k_attn_rows(const AtBwd a)
             dot = lanes_sum_dpp<kLanes>(dot);
             if (part == 0 && tile < a.order.tiles) a.w.info[(int64_t(head) * a.order.tiles + tile) * (kAbWords * 32) + kAbDelta * 32 + (y & 31)] = __float_as_uint(-dot);
             if (AtNum<T>::kHalf) {
-                most = fmaxf(most, lanes_sum_dpp<kLanes>(ss));
-                most_delta = fmaxf(most_delta, fabsf(dot));
+                ss = lanes_sum_dpp<kLanes>(ss);
+                if (ss < __builtin_inff()) most = fmaxf(most, ss);             // not finite: keys that the row sees get no better, others are to
+                if (fabsf(dot) < __builtin_inff()) most_delta = fmaxf(most_delta, fabsf(dot));
             }
         }
     }

@@ -38,7 +38,8 @@ AtShape at_shape(const mesa_attention &a, const mesa_attention_mask &m)
 // A workgroup takes kAtStretch consecutive queries of a sequence, whose places are consecutive keys.  Documents: where the number
 // changes within the stretch is one bit per place in LDS, and each query finds its run's ends among those; only the run that the
 // first place lies in, and the one of the last, may reach out of the stretch, and two waves search for those ends, 64 keys at a time.
-// Every query searching for itself took 51 us where this takes 14 (64 x 32768 queries, 61 documents a row).
+// Every query searching for itself took 51 us where this takes 8.8 (64 x 32768 queries, 61 documents a row; 63 such rows 10.7), of which 5.4 are
+// spent without documents: 16.8 MB written, as fast as memory takes them.
 constexpr int kAtStretch = 1024;
 
 // the first x of [l, h] with x == h or not below(x), for a row where below() holds up to there and no further; 64 probes a round
@@ -60,28 +61,27 @@ template <typename Below> __device__ __forceinline__ int at_search(int l, int h,
 }
 
 template <bool DOC>
-__global__ __launch_bounds__(kThreads) void k_attn_bounds(int32_t *__restrict__ lo, int32_t *__restrict__ hi, int Nq, int Nk, int causal, int64_t window,
+__global__ __launch_bounds__(kThreads) void k_attn_bounds(int32_t *__restrict__ lo, int32_t *__restrict__ hi, int Nq, int Nk, int causal, int window,
                                                           const int32_t *__restrict__ kv_len, const int32_t *__restrict__ q_start, const int32_t *__restrict__ prefix,
-                                                          const int32_t *__restrict__ doc, uint32_t per)
+                                                          const int32_t *__restrict__ doc, uint32_t B)
 {
     constexpr int kU = kAtStretch / kThreads, kWords = kAtStretch / 64;
     __shared__ uint64_t change[kWords];
     __shared__ int end[2];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t b = blockIdx.x / per;
-    const int i0 = int(blockIdx.x - uint32_t(b) * per) * kAtStretch;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    const int64_t b = blockIdx.x % uint32_t(B);     // the sequences first: where they are a multiple of 8, a sequence's workgroups share one XCD's cache
+    const int i0 = int(blockIdx.x / uint32_t(B)) * kAtStretch, count = Nq - i0 < kAtStretch ? Nq - i0 : kAtStretch;
     int n = Nk;
     if (kv_len) n = kv_len[b] < n ? kv_len[b] : n;
-    const int64_t p0 = (q_start ? int64_t(q_start[b]) : int64_t(Nk) - Nq) + i0;      // the place of the stretch's first query
-    const int64_t p1 = p0 + (Nq - i0 < kAtStretch ? Nq - i0 : kAtStretch) - 1;
-    const int first = int(p0 > 0 ? p0 : 0), last = int(p1 < n - 1 ? p1 : n - 1);      // those among the keys: first..last, if any (p0 <= n - 1 then)
-    const bool some = n > 0 && p0 < n && p1 >= 0;
+    const int64_t from = (q_start ? int64_t(q_start[b]) : int64_t(Nk) - Nq) + i0;    // the place of the stretch's first query
+    const bool some = n > 0 && from < n && from + count > 0;                           // of any of its queries among the keys; -kAtStretch < from < n then, and 32 bits do
+    const int p0 = some ? int(from) : 0, p1 = p0 + count - 1, first = p0 > 0 ? p0 : 0, last = p1 < n - 1 ? p1 : n - 1;
     const int32_t *d = DOC ? doc + b * Nk : nullptr;
     uint32_t words = 0;
     if (DOC && some) {
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
-            const int64_t x = p0 + u * kThreads + threadIdx.x;
+            const int x = p0 + u * kThreads + int(threadIdx.x);
             const bool differs = x > first && x <= last && d[x] != d[x - 1];
             const uint64_t m = __ballot(differs);
             if (lane == 0) change[u * (kThreads / 64) + wave] = m;
@@ -99,44 +99,45 @@ __global__ __launch_bounds__(kThreads) void k_attn_bounds(int32_t *__restrict__ 
     const int top = prefix ? prefix[b] : 0;
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-        const int k = u * kThreads + threadIdx.x;
-        if (i0 + k >= Nq) break;
-        const int64_t p = p0 + k;
-        int64_t l = 0, h = 0;
-        if (p >= 0 && p < n) {
+        const int w = u * (kThreads / 64) + wave, k = w * 64 + lane;
+        if (k >= count) break;
+        const int p = p0 + k;
+        int l = 0, h = 0;
+        if (some && p >= 0 && p < n) {
             h = n;
             if (causal) {
-                const int64_t seen = p + 1 > top ? p + 1 : top;
+                const int seen = p + 1 > top ? p + 1 : top;
                 h = seen < h ? seen : h;
             }
             if (window > 0) {
                 l = p - window + 1 > 0 ? p - window + 1 : 0;
                 if (!causal && p + window < h) h = p + window;
             }
-            if (DOC) {
-                const int w = k >> 6, bit = k & 63;
-                const uint64_t c = change[w], below = c & (~uint64_t(0) >> (63 - bit)), above = bit == 63 ? 0 : c >> (bit + 1);
-                const uint32_t before = words & ((1u << w) - 1), behind = words >> w >> 1;
-                int64_t x = end[0], y = end[1];
-                if (below) {
-                    x = p0 + w * 64 + 63 - __clzll(below);
-                } else if (before) {
-                    const int v = 31 - __clz(before);
-                    x = p0 + v * 64 + 63 - __clzll(change[v]);
-                }
-                if (above) {
-                    y = p + 1 + __builtin_ctzll(above);
-                } else if (behind) {
-                    const int v = w + 1 + __builtin_ctz(behind);
-                    y = p0 + v * 64 + __builtin_ctzll(change[v]);
-                }
-                l = x > l ? x : l;
-                h = y < h ? y : h;
-            }
-            if (l >= h) l = h = 0;
         }
-        lo[b * Nq + i0 + k] = int32_t(l);
-        hi[b * Nq + i0 + k] = int32_t(h);
+        if (DOC && some) {
+            // the last change among the words before and the first among those behind: one answer per wave; then this word's own
+            const uint64_t c = uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(change[w] >> 32))))) << 32 | uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(change[w]))));
+            const uint32_t before = words & ((1u << w) - 1), behind = words >> w >> 1;
+            int x = end[0], y = end[1];
+            if (before) {
+                const int v = 31 - __clz(before);
+                x = p0 + v * 64 + 63 - __clzll(change[v]);
+            }
+            if (behind) {
+                const int v = w + 1 + __builtin_ctz(behind);
+                y = p0 + v * 64 + __builtin_ctzll(change[v]);
+            }
+            if (c) {
+                const uint64_t below = c & (~uint64_t(0) >> (63 - lane)), above = c & ~(~uint64_t(0) >> (63 - lane));
+                if (below) x = p0 + w * 64 + 63 - __clzll(below);
+                if (above) y = p0 + w * 64 + __builtin_ctzll(above);
+            }
+            l = x > l ? x : l;
+            h = y < h ? y : h;
+        }
+        if (l >= h) l = h = 0;
+        lo[b * Nq + i0 + k] = l;
+        hi[b * Nq + i0 + k] = h;
     }
 }
 
@@ -321,11 +322,11 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 && !BIAS ? 4 : 2) v
     }
 
     l = at_pair_sum(l);
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;       // not a number where a score is none, lse then too
     if (r_own >= s.R) return;
     if (a.part_o) {
         const int64_t at = int64_t(split) * a.heads * s.R + int64_t(head) * s.R + r;
-        if (half == 0) a.part_lse[at] = l > 0.0f ? m + __log2f(l) : -__builtin_inff();
+        if (half == 0) a.part_lse[at] = l == 0.0f ? -__builtin_inff() : m + __log2f(l);
 #pragma unroll
         for (int d = 0; d < kDt; ++d)
 #pragma unroll
@@ -335,7 +336,7 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 && !BIAS ? 4 : 2) v
             }
         return;
     }
-    if (half == 0) a.lse[(int64_t(b) * s.Hq + hq) * s.Nq + row.token] = l > 0.0f ? (m + __log2f(l)) * kLn2 : -__builtin_inff();
+    if (half == 0) a.lse[(int64_t(b) * s.Hq + hq) * s.Nq + row.token] = l == 0.0f ? -__builtin_inff() : (m + __log2f(l)) * kLn2;
     char *op = a.o.p + int64_t(b) * a.o.batch + int64_t(row.token) * a.o.token + int64_t(hq) * a.o.head;
 #pragma unroll
     for (int d = 0; d < kDt; ++d)
@@ -403,13 +404,13 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(const AtFwd a)
 #pragma unroll
         for (int k = 0; k < 4; ++k) x[k] = fmaf(w, sums[g][quad][k], x[k]);
     }
-    const float inv = total > 0.0f ? 1.0f / total : 0.0f;
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
     const uint32_t head = uint32_t(at / s.R), r = uint32_t(at - int64_t(head) * s.R);
     const int b = int(head) / s.Hk, hk = int(head) - b * s.Hk;
     const AtRow row = at_row(s, r);
     const int hq = hk * s.G + int(row.g);
     at_store4<T>(a.o.p + int64_t(b) * a.o.batch + int64_t(row.token) * a.o.token + int64_t(hq) * a.o.head + e * 2, x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-    if (e == 0) a.lse[(int64_t(b) * s.Hq + hq) * s.Nq + row.token] = total > 0.0f ? (m + __log2f(total)) * kLn2 : -__builtin_inff();
+    if (e == 0) a.lse[(int64_t(b) * s.Hq + hq) * s.Nq + row.token] = total == 0.0f ? -__builtin_inff() : (m + __log2f(total)) * kLn2;
 }
 
 struct AtFwdPlan {
@@ -480,7 +481,7 @@ extern "C" MESA_EXPORT mesa_status mesa_attention_bounds(int32_t *lo, int32_t *h
     if (Nq >= top || Nk >= top || B >= (int64_t(1) << 40) / Nq || B * ceil_div(Nq, kAtStretch) > most_workgroups(kThreads)) return MESA_ERR_UNSUPPORTED;
     const uint32_t per = uint32_t(ceil_div(Nq, kAtStretch));
     hipLaunchKernelGGL(doc ? k_attn_bounds<true> : k_attn_bounds<false>, dim3(uint32_t(B) * per), dim3(kThreads), 0, static_cast<hipStream_t>(stream), lo, hi, int(Nq), int(Nk),
-                       causal, window < top ? window : top, kv_len, q_start, prefix, doc, per);
+                       causal, int(window < top ? window : top), kv_len, q_start, prefix, doc, uint32_t(B));
     return launch_status();
 }
 

@@ -226,6 +226,61 @@ def test_what_nobody_sees_does_not_matter(junk, dtype):
         assert (g[dead] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("Nq,Nk", [(100, 300), (3, 4000)])
+def test_what_is_not_a_number_stays_so(Nq, Nk, cap, dtype):
+    """a query that is not a number, and one that sees a key that is none: o and lse are none there, and as they were in other rows"""
+    a = m.Attention(1, Nq, Nk, 2, 1, 64, 0.125, cap)
+    q, k, v, _ = tensors(1, Nq, Nk, 2, 1, 64, dtype, "bnhd", 9)
+    lo = torch.zeros(1, Nq, dtype=torch.int32, device=DEV)
+    hi = torch.full_like(lo, Nk - 100)
+    hi[0, 2] = Nk
+    o, lse = forward(a, q, k, v, lo, hi, None, None)
+    q[0, 1, 0, 5] = math.nan
+    k[0, Nk - 50, 0, 3] = math.nan
+    got, glse = forward(a, q, k, v, lo, hi, None, None)
+    bad = torch.zeros(1, Nq, 2, dtype=torch.bool, device=DEV)
+    bad[0, 1, 0] = True
+    bad[0, 2] = True
+    assert torch.isnan(got[bad]).all() and torch.equal(got[~bad], o[~bad])
+    bad = bad.transpose(1, 2)
+    assert torch.isnan(glse[bad]).all() and torch.equal(glse[~bad], lse[~bad])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_infinite_scores_meet_the_cap(dtype):
+    """tanh of 3e4 / 8 / 20 is one in 64 bits already, so an infinity in that place changes nothing"""
+    a = m.Attention(1, 70, 130, 2, 1, 64, 0.125, 20.0)
+    q, k, v, _ = tensors(1, 70, 130, 2, 1, 64, dtype, "bnhd", 10)
+    q[..., 7] = q[..., 7].sign() + (q[..., 7] == 0)
+    for sign in (1, -1):
+        k[0, 77, 0, 7] = sign * 3e4
+        want = forward(a, q, k, v, None, None, None, None)
+        k[0, 77, 0, 7] = sign * math.inf
+        got = forward(a, q, k, v, None, None, None, None)
+        assert all(torch.equal(g, w) for g, w in zip(got, want)) and torch.isfinite(got[0]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("junk", [math.nan, math.inf])
+def test_a_gradient_that_is_no_number_stays_with_what_it_meets(junk, dtype):
+    """two documents of which one has an infinity in its gradient: the other one's gradients are what they were without"""
+    a = m.Attention(1, 192, 192, 2, 1, 64, 0.125)
+    q, k, v, do = tensors(1, 192, 192, 2, 1, 64, dtype, "bnhd", 11)
+    lo = torch.tensor([[0] * 64 + [64] * 128], dtype=torch.int32, device=DEV)
+    hi = torch.tensor([[64] * 64 + [192] * 128], dtype=torch.int32, device=DEV)
+    seen = torch.zeros(1, 192, 192, dtype=torch.bool, device=DEV)
+    seen[0, :64, :64] = True
+    seen[0, 64:, 64:] = True
+    o, lse = forward(a, q, k, v, lo, hi, None, None)
+    want, bound = attention_bwd(q, k, v, o, lse, do, a.scale, 0, None, torch.zeros(1, dtype=torch.int32, device=DEV), seen)
+    do[0, 20, 1, 9] = junk
+    for g, w, b, n in zip(backward(a, q, k, v, o, lse, do, lo, hi, None, None), want, bound, ("dq", "dk", "dv")):
+        check(g[:, 64:], w[:, 64:], b[:, 64:], n)
+        assert not torch.isfinite(g[:, 20 if n == "dq" else slice(0, 64)]).all(), n
+
+
 def test_intervals_beyond_the_keys_are_cut():
     a = m.Attention(1, 70, 50, 2, 2, 32, 0.3)
     q, k, v, _ = tensors(1, 70, 50, 2, 2, 32, torch.float16, "bnhd", 6)
