@@ -2,8 +2,8 @@
 //   p = exp(s - lse),  delta_i = do_i.o_i,  ds = p (do.v - delta) (times the cap's derivative 1 - tanh^2)
 //   dv_j = sum_i p_ij do_i,   dk_j = scale sum_i ds_ij q_i,   dq_i = scale sum_j ds_ij k_j
 //
-// Four steps on the stream: codes become 16-bit operands in the workspace (they are read many times over); a pass over
-// the rows leaves delta, log-sum-exps and intervals, row by row; then keys (dk and dv: a wave owns 32 keys and walks over
+// Three steps on the stream: a pass over the rows leaves delta, log-sum-exps and intervals, row by row, and turns codes into 16-bit
+// operands in the workspace (they are read many times over); then keys (dk and dv: a wave owns 32 keys and walks over
 // the rows) and queries (dq: a wave owns 32 rows and walks over the keys).  The scores are formed in both, seven products instead
 // of five: dq added up across workgroups would need atomics, whose order changes the result.  A group's heads are rows of
 // the same walk, so the gradients of a shared key head add up in registers.
@@ -67,7 +67,7 @@ struct AtBwd {
     uint32_t heads, key_blocks, splits, row_blocks;
 };
 
-// codes to contiguous (B, heads, tokens, D) elements, as mesa_dequantize; eight per thread, up to three operands in one launch
+// codes to contiguous (B, heads, tokens, D) elements, as mesa_dequantize; eight per thread
 struct AbCodes {
     AtView q;
     const float *alpha, *beta;
@@ -76,19 +76,13 @@ struct AbCodes {
     uint32_t first, per_head;          // workgroups: the operand's first one, those of a (sequence, head)
 };
 struct AbOperands {
-    AbCodes c[3];
-    int32_t count, D;
+    AbCodes c[3], v;                   // v: values that the row pass has to read anyway
+    int32_t count;
+    bool values;
     FastDiv div_d;                     // by D / 8
 };
-template <typename T> __global__ __launch_bounds__(kThreads) void k_attn_operand(const AbOperands a)
+template <typename T> __device__ __forceinline__ typename Store<T>::raw_t ab_operand(const AbCodes &c, int D, uint32_t b, uint32_t h, uint32_t t, uint32_t e)
 {
-    int n = 0;
-    if (a.count > 1 && blockIdx.x >= a.c[1].first) n = 1;
-    if (a.count > 2 && blockIdx.x >= a.c[2].first) n = 2;
-    const AbCodes &c = n == 0 ? a.c[0] : n == 1 ? a.c[1] : a.c[2];
-    const uint32_t blk = blockIdx.x - c.first, bh = blk / c.per_head, b = bh / uint32_t(c.heads), h = bh - b * uint32_t(c.heads);
-    const uint32_t i = (blk - bh * c.per_head) * kThreads + threadIdx.x, t = fastdiv(i, a.div_d), e = (i - t * uint32_t(a.D / 8)) * 8;
-    if (t >= uint32_t(c.tokens)) return;
     const u32x2 v = *reinterpret_cast<const u32x2 *>(c.q.p + int64_t(b) * c.q.batch + int64_t(t) * c.q.token + int64_t(h) * c.q.head + e);
     float f[8];
     codes_to_float(v, f);
@@ -98,16 +92,29 @@ template <typename T> __global__ __launch_bounds__(kThreads) void k_attn_operand
         const float y = f[k] * s;
         f[k] = y + z;
     }
-    Store<T>::store(c.out, (int64_t(bh) * c.tokens + t) * a.D + e, Store<T>::pack(f));
+    const typename Store<T>::raw_t r = Store<T>::pack(f);
+    Store<T>::store(c.out, ((int64_t(b) * c.heads + h) * c.tokens + t) * D + e, r);
+    return r;
 }
 
 // The row pass.  Workgroups [0, blocks) of a head: the deltas of 128 places, log-sum-exps, intervals and the summaries of their four
-// tiles; further ones (binary16): the largest norm of 128 keys' values.  Eight or sixteen lanes per row.
+// tiles; further ones (binary16): the largest norm of 128 keys' values, which become elements there if they are codes.  Eight or sixteen
+// lanes per row.  Behind all heads' the workgroups of the other operands that are codes.
 template <typename T, int DP>
-__global__ __launch_bounds__(kThreads) void k_attn_rows(const AtBwd a)
+__global__ __launch_bounds__(kThreads) void k_attn_rows(const AtBwd a, const AbOperands in)
 {
     constexpr int kLanes = DP / 8, kPer = kThreads / kLanes;
     const AtShape &s = a.s;
+    const uint32_t mine = a.heads * (a.w.blocks + (AtNum<T>::kHalf ? a.w.key_blocks : 0));
+    if (blockIdx.x >= mine) {
+        const uint32_t at = blockIdx.x - mine;
+        const int n = in.count > 2 && at >= in.c[2].first ? 2 : in.count > 1 && at >= in.c[1].first ? 1 : 0;
+        const AbCodes &c = n == 0 ? in.c[0] : n == 1 ? in.c[1] : in.c[2];
+        const uint32_t blk = at - c.first, bh = blk / c.per_head, b = bh / uint32_t(c.heads), h = bh - b * uint32_t(c.heads);
+        const uint32_t i = (blk - bh * c.per_head) * kThreads + threadIdx.x, t = fastdiv(i, in.div_d), e = (i - t * uint32_t(s.D / 8)) * 8;
+        if (t < uint32_t(c.tokens)) ab_operand<T>(c, s.D, b, h, t, e);
+        return;
+    }
     const uint32_t head = blockIdx.x % a.heads, blk = blockIdx.x / a.heads;
     const int b = int(head / uint32_t(s.Hk)), hk = int(head) - b * s.Hk;
     const int tid = threadIdx.x, part = tid % kLanes, first = tid / kLanes;
@@ -120,7 +127,8 @@ __global__ __launch_bounds__(kThreads) void k_attn_rows(const AtBwd a)
             float ss = 0.0f;
             if (j < s.Nk && part * 8 < s.D) {
                 float f[8];
-                Store<T>::unpack(Store<T>::load(a.v.p + int64_t(b) * a.v.batch + int64_t(j) * a.v.token + int64_t(hk) * a.v.head, part * 8), f);
+                Store<T>::unpack(in.values ? ab_operand<T>(in.v, s.D, uint32_t(b), uint32_t(hk), uint32_t(j), uint32_t(part) * 8)
+                                                : Store<T>::load(a.v.p + int64_t(b) * a.v.batch + int64_t(j) * a.v.token + int64_t(hk) * a.v.head, part * 8), f);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) ss = fmaf(f[k], f[k], ss);
             }
@@ -235,8 +243,7 @@ template <bool CAP> __device__ __forceinline__ float ab_score(const AtShape &s, 
 // ---------------------------------------------------------------------------------------------
 // dq: a wave owns 32 rows
 // ---------------------------------------------------------------------------------------------
-template <typename T, int DP, int NW, int BN, bool CAP, bool BIAS, bool FINE>
-__global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
+template <typename T, int DP, int NW, int BN, bool CAP, bool BIAS, bool FINE> __device__ __forceinline__ void ab_dq(const AtBwd &a, uint32_t block)
 {
     typedef AtNum<T> Num;
     typedef AtTile<NW * 64, BN, DP> Tile;
@@ -246,7 +253,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
     __shared__ uint64_t seen[NW];
     const AtShape &s = a.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), half = lane >> 5;
-    const uint32_t head = blockIdx.x % a.heads, rb = a.row_blocks - 1 - blockIdx.x / a.heads;
+    const uint32_t head = block % a.heads, rb = a.row_blocks - 1 - block / a.heads;
     const int b = int(head / uint32_t(s.Hk)), hk = int(head) - b * s.Hk;
     const uint32_t r_own = (rb * NW + wave) * 32 + (lane & 31), r = r_own < s.R ? r_own : s.R - 1;
     const AtRow row = at_row(s, r);
@@ -285,6 +292,18 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
     }
     const int t0 = __builtin_amdgcn_readfirstlane(bhi > 0 ? blo / BN : 0), t1 = __builtin_amdgcn_readfirstlane(bhi > 0 ? (bhi + BN - 1) / BN : 0);
 
+    const char *kbase = a.k.p + int64_t(b) * a.k.batch + int64_t(hk) * a.k.head, *vbase = a.v.p + int64_t(b) * a.v.batch + int64_t(hk) * a.v.head;
+    Tile tk, tv;
+    const uint32_t k_step = uint32_t(a.k.token), v_step = uint32_t(a.v.token), k_at = Tile::place(k_step, s.D), v_at = Tile::place(v_step, s.D);
+    kbase += int64_t(t0) * BN * a.k.token;
+    vbase += int64_t(t0) * BN * a.v.token;
+    auto fetch = [&](int t) __attribute__((always_inline)) {        // t0, t0 + 1, ...
+        tk.load(kbase, s.Nk - t * BN, k_step, s.D, k_at);
+        tv.load(vbase, s.Nk - t * BN, v_step, s.D, v_at);
+        kbase += int64_t(BN) * a.k.token;
+        vbase += int64_t(BN) * a.v.token;
+    };
+    if (t0 < t1) fetch(t0);
     float undo = s.scale;                             // of the sums; the factor of ds goes into p, which nothing else here takes
     if (Num::kHalf) {
         float ss = 0.0f, vmax = 0.0f;
@@ -302,17 +321,6 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
         undo = s.scale * ab_pow2(-e);
     }
 
-    const char *kbase = a.k.p + int64_t(b) * a.k.batch + int64_t(hk) * a.k.head, *vbase = a.v.p + int64_t(b) * a.v.batch + int64_t(hk) * a.v.head;
-    Tile tk, tv;
-    const uint32_t k_step = uint32_t(a.k.token), v_step = uint32_t(a.v.token), k_at = Tile::place(k_step, s.D), v_at = Tile::place(v_step, s.D);
-    kbase += int64_t(t0) * BN * a.k.token;
-    vbase += int64_t(t0) * BN * a.v.token;
-    auto fetch = [&](int t) __attribute__((always_inline)) {        // t0, t0 + 1, ...
-        tk.load(kbase, s.Nk - t * BN, k_step, s.D, k_at);
-        tv.load(vbase, s.Nk - t * BN, v_step, s.D, v_at);
-        kbase += int64_t(BN) * a.k.token;
-        vbase += int64_t(BN) * a.v.token;
-    };
     at_acc dq[kDt];
 #pragma unroll
     for (int d = 0; d < kDt; ++d)
@@ -376,7 +384,6 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
                 }
         }
     };
-    if (t0 < t1) fetch(t0);
     for (int t = t0, cur = 0; t < t1; ++t, cur ^= 1) {
         char *lk = lds + cur * 2 * Tile::kBytes, *lv = lk + Tile::kBytes;
         const int j0 = t * BN;
@@ -411,8 +418,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attn_dq(const AtBwd a)
 // ---------------------------------------------------------------------------------------------
 // A step is two tiles of 32 rows.  Where a tile lies at the edge of what its rows see, probabilities are set to zero element by
 // element; rows that see nothing are zeros in LDS, so that what they hold does not enter.
-template <typename T, int DP, bool CAP, bool BIAS, bool FINE>
-__global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd a)
+template <typename T, int DP, bool CAP, bool BIAS, bool FINE> __device__ __forceinline__ void ab_dkv(const AtBwd &a, uint32_t block)
 {
     typedef AtNum<T> Num;
     constexpr int kKs = DP / 16, kDt = DP / 32, kPieces = DP / 8;
@@ -424,7 +430,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
     const AtShape &s = a.s;
     const AbOrder &order = a.order;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-    const uint32_t head = blockIdx.x % a.heads, rest = blockIdx.x / a.heads, split = rest % a.splits, kb = rest / a.splits;   // the keys that most rows see first
+    const uint32_t head = block % a.heads, rest = block / a.heads, split = rest % a.splits, kb = rest / a.splits;   // the keys that most rows see first
     const int b = int(head / uint32_t(s.Hk)), hk = int(head) - b * s.Hk;
     const int k0 = int(kb) * kAbKeys, j0 = k0 + wave * 32, j_own = j0 + (lane & 31), j = j_own < s.Nk ? j_own : s.Nk - 1;
     u32x4 kf[kKs], vf[kKs];
@@ -624,10 +630,12 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    float2 first_most = make_float2(0.0f, 0.0f);
+    if (Num::kHalf && uint32_t(lane) < a.w.blocks) first_most = a.w.most[int64_t(head) * a.w.blocks + lane];
     int t = __builtin_amdgcn_readfirstlane(next());
     if (t >= 0) fetch(t);                            // on its way while the factors below are formed
     if (Num::kHalf) {
-        float ss = 0.0f, most = 0.0f, most_delta = 0.0f;
+        float ss = 0.0f, most = first_most.x, most_delta = first_most.y;
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks) {
             float f[8];
@@ -636,7 +644,7 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
             for (int k = 0; k < 8; ++k) ss = fmaf(f[k], f[k], ss);
         }
         ss = at_pair_sum(ss);
-        for (uint32_t k = lane; k < a.w.blocks; k += 64) {
+        for (uint32_t k = lane + 64; k < a.w.blocks; k += 64) {
             const float2 m = a.w.most[int64_t(head) * a.w.blocks + k];
             most = fmaxf(most, m.x);
             most_delta = fmaxf(most_delta, m.y);
@@ -710,6 +718,27 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd 
                 at_store4<T>(pv + e * 2, dv[d][4 * w] * undo_v, dv[d][4 * w + 1] * undo_v, dv[d][4 * w + 2] * undo_v, dv[d][4 * w + 3] * undo_v);
             }
         }
+}
+
+// Up to 64 elements a wave of either walk fits two to a SIMD, so that one launch can have both: the rows' workgroups fill in where the
+// keys' run out (8 x 12 heads of 197 keys 23.6 -> 15.1 us, 32 x 12 46.2 -> 44.1).  With many workgroups there is nothing to fill in, and dq
+// alone has more waves (4 x 4 heads of 4001 keys: 390 us in two launches, 402 in one).
+template <typename T, bool CAP, bool BIAS, bool FINE>
+__global__ __launch_bounds__(256, 2) void k_attn_both(const AtBwd a)
+{
+    const uint32_t keys = a.heads * a.key_blocks * a.splits;
+    if (blockIdx.x < keys) ab_dkv<T, 64, CAP, BIAS, FINE>(a, blockIdx.x);
+    else ab_dq<T, 64, 4, 32, CAP, BIAS, FINE>(a, blockIdx.x - keys);
+}
+template <typename T, int DP, bool CAP, bool BIAS, bool FINE>
+__global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd a)
+{
+    ab_dkv<T, DP, CAP, BIAS, FINE>(a, blockIdx.x);
+}
+template <typename T, int DP, bool CAP, bool BIAS, bool FINE>
+__global__ __launch_bounds__(256, 2) void k_attn_dq(const AtBwd a)
+{
+    ab_dq<T, DP, 4, 32, CAP, BIAS, FINE>(a, blockIdx.x);
 }
 
 // the splits added up in their order, four elements of dk or dv per thread
@@ -790,14 +819,18 @@ static AtBwdPlan at_bwd_plan(const mesa_attention &a, const bool codes[3])
 
 template <typename T, int DP, bool CAP, bool BIAS, bool FINE> static mesa_status at_bwd_launch(const AtBwd &a, hipStream_t s)
 {
-    hipLaunchKernelGGL((k_attn_dkv<T, DP, CAP, BIAS, FINE>), dim3(a.heads * a.key_blocks * a.splits), dim3(256), 0, s, a);
+    const uint32_t keys = a.heads * a.key_blocks * a.splits, rows = a.heads * a.row_blocks;
+    const bool both = DP == 64 && keys < 1024;         // two rounds of workgroups
+    if (both) hipLaunchKernelGGL((k_attn_both<T, CAP, BIAS, FINE>), dim3(keys + rows), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_attn_dkv<T, DP, CAP, BIAS, FINE>), dim3(keys), dim3(256), 0, s, a);
     if (const mesa_status st = launch_status()) return st;
     if (a.splits > 1) {
         const int64_t pieces = int64_t(a.heads) * a.s.Nk * (a.s.D / 2);
         hipLaunchKernelGGL(k_attn_add<T>, dim3(uint32_t(ceil_div(pieces, kThreads))), dim3(kThreads), 0, s, a, pieces);
         if (const mesa_status st = launch_status()) return st;
     }
-    hipLaunchKernelGGL((k_attn_dq<T, DP, 4, 32, CAP, BIAS, FINE>), dim3(a.heads * a.row_blocks), dim3(256), 0, s, a);
+    if (both) return MESA_OK;
+    hipLaunchKernelGGL((k_attn_dq<T, DP, CAP, BIAS, FINE>), dim3(rows), dim3(256), 0, s, a);
     return launch_status();
 }
 // Up to kAbFine keys the call is bound by what it reads and writes (14 products of 64 keys to a row's four vectors), and with so few terms to
@@ -807,9 +840,9 @@ template <typename T, int DP, bool CAP, bool BIAS> static mesa_status at_bwd_par
 {
     return a.s.Nk <= kAbFine ? at_bwd_launch<T, DP, CAP, BIAS, true>(a, s) : at_bwd_launch<T, DP, CAP, BIAS, false>(a, s);
 }
-template <typename T, int DP> static mesa_status at_bwd_forms(const AtBwd &a, bool cap, bool bias, hipStream_t s)
+template <typename T, int DP> static mesa_status at_bwd_forms(const AtBwd &a, const AbOperands &in, uint32_t in_blocks, bool cap, bool bias, hipStream_t s)
 {
-    hipLaunchKernelGGL((k_attn_rows<T, DP>), dim3(a.heads * (a.w.blocks + (AtNum<T>::kHalf ? a.w.key_blocks : 0))), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((k_attn_rows<T, DP>), dim3(a.heads * (a.w.blocks + (AtNum<T>::kHalf ? a.w.key_blocks : 0)) + in_blocks), dim3(kThreads), 0, s, a, in);
     if (const mesa_status st = launch_status()) return st;
     if (cap && bias) return at_bwd_parts<T, DP, true, true>(a, s);
     if (cap) return at_bwd_parts<T, DP, true, false>(a, s);
@@ -837,12 +870,12 @@ static mesa_status at_bwd(const mesa_attention &m, AtBwd &a, const AtBwdPlan &p,
     char *out = ws + p.info + p.part;
     AbOperands ops;
     ops.count = 0;
-    ops.D = int32_t(m.D);
+    ops.values = false;
     ops.div_d = make_fastdiv(uint32_t(m.D / 8));
     int64_t blocks = 0;
     for (int k = 0; k < 3; ++k) {
         if (!codes[k]) continue;
-        AbCodes &c = ops.c[ops.count++];
+        AbCodes c;
         c.q = AtView{static_cast<const char *>(in[k].data), in[k].batch, in[k].token, in[k].head};
         c.alpha = in[k].alpha;
         c.beta = in[k].beta;
@@ -851,15 +884,17 @@ static mesa_status at_bwd(const mesa_attention &m, AtBwd &a, const AtBwdPlan &p,
         c.tokens = int32_t(tokens[k]);
         c.first = uint32_t(blocks);
         c.per_head = uint32_t(ceil_div(tokens[k] * (m.D / 8), kThreads));
-        blocks += m.B * heads[k] * int64_t(c.per_head);
+        if (k == 2 && AtNum<T>::kHalf) {
+            ops.v = c;
+            ops.values = true;
+        } else {
+            ops.c[ops.count++] = c;
+            blocks += m.B * heads[k] * int64_t(c.per_head);
+        }
         *view[k] = AtView{out, heads[k] * tokens[k] * m.D * 2, m.D * 2, tokens[k] * m.D * 2};
         out += p.operand[k];
     }
-    if (ops.count) {
-        hipLaunchKernelGGL(k_attn_operand<T>, dim3(uint32_t(blocks)), dim3(kThreads), 0, s, ops);
-        if (const mesa_status st = launch_status()) return st;
-    }
-    return m.D <= 64 ? at_bwd_forms<T, 64>(a, m.cap > 0.0f, bias, s) : at_bwd_forms<T, 128>(a, m.cap > 0.0f, bias, s);
+    return m.D <= 64 ? at_bwd_forms<T, 64>(a, ops, uint32_t(blocks), m.cap > 0.0f, bias, s) : at_bwd_forms<T, 128>(a, ops, uint32_t(blocks), m.cap > 0.0f, bias, s);
 }
 
 }  // namespace mesa
@@ -898,7 +933,7 @@ extern "C" MESA_EXPORT mesa_status mesa_attention_bwd_q(mesa_attention a, mesa_a
         return MESA_ERR_INVALID_ARG;
     const AtBwdPlan p = at_bwd_plan(a, codes);
     const int64_t heads = a.B * a.Hk, most = most_workgroups(256), rows = heads * a.Nq * group, keys = heads * a.Nk, operands = (rows + 2 * keys) * (a.D / 8) / kThreads + heads * (group + 2);
-    if (heads * p.key_blocks * p.splits > most || heads * (int64_t(p.blocks) + p.key_blocks) > most || heads * p.row_blocks > most || operands > most ||
+    if (heads * (int64_t(p.key_blocks) * p.splits + p.row_blocks) > most || heads * (int64_t(p.blocks) + p.key_blocks) + operands > most ||
         (rows > 2 * keys ? rows : 2 * keys) * (a.D / 4) > most * kThreads)
         return MESA_ERR_UNSUPPORTED;
     if (a.Nq > 0 && a.Nk > 0 && (!ws || !aligned16(ws) || ws_bytes < p.total)) return MESA_ERR_WORKSPACE;
