@@ -154,7 +154,13 @@ struct AtFwd {
 };
 
 // NW waves of 32 rows, tiles of BN keys
-template <typename T, int DP, int NW, int BN, bool CAP, bool BIAS>
+// CAP: kAtCapped takes at_tanh<true>.  kAtCappedLong leaves r = -1 / (2^u + 1) in a score's place, u = 2 log2(e) s / cap, whose score is
+// cap + 2 cap r: both go into the exponent's one multiply-add, three instructions less of eleven a score where vector instructions are
+// what binds (2 x 8192 x 16 heads of 128 717 -> 670 us, of 64 486 -> 423).  Such a score is off by 2^-23 of the cap or so, whatever its
+// size; lse over 600 keys then by 1.3e-7 of itself (4e-8 with tanh), where a query sees one key of them by 1.5e-6: so only from kAtLong keys on.
+enum { kAtUncapped = 0, kAtCapped, kAtCappedLong };
+constexpr int kAtLong = 512;
+template <typename T, int DP, int NW, int BN, int CAP, bool BIAS>
 __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 && !BIAS ? 4 : 2) void k_attn_fwd(const AtFwd a)
 {
     typedef AtNum<T> Num;
@@ -190,7 +196,8 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 && !BIAS ? 4 : 2) v
     }
     const float slope2 = BIAS ? s.slopes[hq] * kLog2e : 0.0f;
     const int place = BIAS ? at_place(s, b, row.token) : 0;
-    const float to_score = CAP ? s.cap2 : s.c;      // to powers of two, from tanh or from the product
+    const float to_score = CAP == kAtCappedLong ? 2.0f * s.cap2 : CAP ? s.cap2 : s.c;      // to powers of two, from r, tanh or the product
+    const float more = CAP == kAtCappedLong ? s.cap2 : 0.0f;
     __syncthreads();
     int blo = 0x7FFFFFFF, bhi = 0, full_lo[NW], full_hi[NW];      // the same of the workgroup's rows; what each wave's rows see, all of them
 #pragma unroll
@@ -249,8 +256,9 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 && !BIAS ? 4 : 2) v
             for (int t = 0; t < kSub; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    if (CAP) x[t][i] = at_tanh<true>(x[t][i] * s.c);
-                    if (BIAS) x[t][i] = fmaf(x[t][i], to_score, -slope2 * fabsf(away - float(t * 32 + at_reg_row(i))));
+                    if (CAP == kAtCappedLong) x[t][i] = __builtin_amdgcn_rcpf(-1.0f - at_exp2(x[t][i] * s.c));
+                    else if (CAP) x[t][i] = at_tanh<true>(x[t][i] * s.c);
+                    if (BIAS) x[t][i] = fmaf(x[t][i], to_score, fmaf(-slope2, fabsf(away - float(t * 32 + at_reg_row(i))), more));
                 }
         }
         if (!whole) {
@@ -266,7 +274,7 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 && !BIAS ? 4 : 2) v
             for (int i = 0; i < 16; ++i) top = fmaxf(top, x[t][i]);
         top = at_pair_max(top);
         constexpr bool kRaw = !BIAS;               // the factor is then still to come (it is positive)
-        if (kRaw) top *= to_score;
+        if (kRaw) top = fmaf(top, to_score, more);
         // the sums are scaled anew only where a row's maximum has grown by more than 2^8: probabilities up to 2^8 are as exact
         if (__ballot(top > m + 8.0f)) {
             const float m1 = fmaxf(m, top), f = at_exp2(m - m1);
@@ -279,6 +287,7 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 && !BIAS ? 4 : 2) v
         }
         u32x4 p[2 * kSub];
         float l1 = 0.0f;
+        const float less = more - m;
 #pragma unroll
         for (int t = 0; t < kSub; ++t)
 #pragma unroll
@@ -286,7 +295,7 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 && !BIAS ? 4 : 2) v
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     const int i = 8 * g + 2 * w;
-                    const float e0 = at_exp2(kRaw ? fmaf(x[t][i], to_score, -m) : x[t][i] - m), e1 = at_exp2(kRaw ? fmaf(x[t][i + 1], to_score, -m) : x[t][i + 1] - m);
+                    const float e0 = at_exp2(kRaw ? fmaf(x[t][i], to_score, less) : x[t][i] - m), e1 = at_exp2(kRaw ? fmaf(x[t][i + 1], to_score, less) : x[t][i + 1] - m);
                     l += e0;
                     l1 += e1;
                     p[2 * t + g][w] = Num::pack(e0, e1);
@@ -443,8 +452,10 @@ static AtFwdPlan at_fwd_plan(const mesa_attention &a)
 template <typename T, int DP, bool CAP, bool BIAS> static void at_fwd_launch(const AtFwd &a, const AtFwdPlan &p, hipStream_t s)
 {
     const dim3 grid(a.heads * a.row_blocks * a.splits);
-    if (p.waves == 1) hipLaunchKernelGGL((k_attn_fwd<T, DP, 1, 32, CAP, BIAS>), grid, dim3(64), 0, s, a);
-    else hipLaunchKernelGGL((k_attn_fwd<T, DP, 4, 64, CAP, BIAS>), grid, dim3(256), 0, s, a);
+    constexpr int kCap = CAP ? kAtCapped : kAtUncapped, kLong = CAP ? kAtCappedLong : kAtUncapped;
+    if (p.waves == 1) hipLaunchKernelGGL((k_attn_fwd<T, DP, 1, 32, kCap, BIAS>), grid, dim3(64), 0, s, a);     // what it reads takes longer
+    else if (a.s.Nk < kAtLong) hipLaunchKernelGGL((k_attn_fwd<T, DP, 4, 64, kCap, BIAS>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_attn_fwd<T, DP, 4, 64, kLong, BIAS>), grid, dim3(256), 0, s, a);
 }
 template <typename T, int DP> static void at_fwd_forms(const AtFwd &a, const AtFwdPlan &p, bool cap, bool bias, hipStream_t s)
 {

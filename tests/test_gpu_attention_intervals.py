@@ -110,6 +110,9 @@ CASES = [  # B, Nq, Nk, Hq, Hk, D, mask, cap, bias, layout
     (2, 21, 37, 66, 2, 24, dict(causal=True, docs=3), 10.0, True, "bnhd"),
     (1, 130, 130, 33, 1, 120, dict(window=20, pad=True), 0, False, "bnhd"),
     (1, 200, 200, 5, 1, 72, {}, 0, False, "packed"),
+    # capped scores over many keys
+    (1, 530, 530, 4, 2, 72, dict(causal=True, prefix=True), 15.0, True, "packed"),
+    (1, 150, 700, 2, 1, 64, dict(causal=True, window=90), 30.0, False, "bnhd"),
 ]
 FEW = [  # few rows over many keys: the keys are shared out
     (1, 1, 5000, 8, 1, 128, dict(causal=True), 0, False, "bnhd"),
@@ -228,7 +231,7 @@ def test_what_nobody_sees_does_not_matter(junk, dtype):
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
 @pytest.mark.parametrize("cap", [0.0, 20.0])
-@pytest.mark.parametrize("Nq,Nk", [(100, 300), (3, 4000)])
+@pytest.mark.parametrize("Nq,Nk", [(100, 300), (3, 4000), (50, 600)])
 def test_what_is_not_a_number_stays_so(Nq, Nk, cap, dtype):
     """a query that is not a number, and one that sees a key that is none: o and lse are none there, and as they were in other rows"""
     a = m.Attention(1, Nq, Nk, 2, 1, 64, 0.125, cap)
@@ -249,10 +252,11 @@ def test_what_is_not_a_number_stays_so(Nq, Nk, cap, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
-def test_infinite_scores_meet_the_cap(dtype):
+@pytest.mark.parametrize("Nk", [130, 530])
+def test_infinite_scores_meet_the_cap(Nk, dtype):
     """tanh of 3e4 / 8 / 20 is one in 64 bits already, so an infinity in that place changes nothing"""
-    a = m.Attention(1, 70, 130, 2, 1, 64, 0.125, 20.0)
-    q, k, v, _ = tensors(1, 70, 130, 2, 1, 64, dtype, "bnhd", 10)
+    a = m.Attention(1, 70, Nk, 2, 1, 64, 0.125, 20.0)
+    q, k, v, _ = tensors(1, 70, Nk, 2, 1, 64, dtype, "bnhd", 10)
     q[..., 7] = q[..., 7].sign() + (q[..., 7] == 0)
     for sign in (1, -1):
         k[0, 77, 0, 7] = sign * 3e4
