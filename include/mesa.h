@@ -479,7 +479,8 @@ typedef struct mesa_attention_mask {
     const int32_t *q_start;      /* [B] or NULL: Nk - Nq */
 } mesa_attention_mask;
 /* (B, tokens, heads, D) in memory: element (b, t, h, d) at b*batch + t*token + h*head + d.  Strides are multiples of 8, data is
- * 16-byte aligned, and the heads of a group and 256 tokens span less than 2^30 elements.  alpha NULL: elements of dt.  Else
+ * 16-byte aligned, and the heads of a group and 256 tokens span less than 2^30 elements.  Operands may share memory in any way (stride 0
+ * for one row that stands for all); results overlap neither operands nor each other nor themselves.  alpha NULL: elements of dt.  Else
  * codes, de-quantized to dt as mesa_dequantize does, with [heads] binary32 alpha and beta (data 8-byte aligned then). */
 typedef struct mesa_attention_in {
     const void *data;

@@ -937,6 +937,14 @@ extern "C" MESA_EXPORT mesa_status mesa_attention_bwd_q(mesa_attention a, mesa_a
         (rows > 2 * keys ? rows : 2 * keys) * (a.D / 4) > most * kThreads)
         return MESA_ERR_UNSUPPORTED;
     if (a.Nq > 0 && a.Nk > 0 && (!ws || !aligned16(ws) || ws_bytes < p.total)) return MESA_ERR_WORKSPACE;
+    if (a.Nq > 0 && a.Nk > 0) {                       // operands are read again after the first results
+        const void *r[3] = {dq.data, dk.data, dv.data}, *x[5] = {q.data, k.data, v.data, o.data, dO.data};
+        for (int n = 0; n < 3; ++n) {
+            if (r[n] == r[(n + 1) % 3]) return MESA_ERR_INVALID_ARG;
+            for (const void *y : x)
+                if (r[n] == y) return MESA_ERR_INVALID_ARG;
+        }
+    }
     AtBwd f;
     f.s = at_shape(a, m);
     auto view = [](const mesa_attention_in &x) { return AtView{static_cast<const char *>(x.data), x.batch * 2, x.token * 2, x.head * 2}; };

@@ -527,6 +527,7 @@ extern "C" MESA_EXPORT mesa_status mesa_attention_fwd(mesa_attention a, mesa_att
     const int64_t groups = a.B * a.Hk, quads = groups * a.Nq * group * (a.D / 4);
     if (groups * p.row_blocks * p.splits > most_workgroups(256) || (p.splits > 1 && groups * a.Nq * group > most_workgroups(kThreads)) || ceil_div(quads, kThreads) > most_workgroups(kThreads)) return MESA_ERR_UNSUPPORTED;
     if (p.ws && (!ws || !aligned16(ws) || ws_bytes < p.ws)) return MESA_ERR_WORKSPACE;
+    if (a.Nk && (o.data == q.data || o.data == k.data || o.data == v.data)) return MESA_ERR_INVALID_ARG;      // other workgroups read them yet
     hipStream_t s = static_cast<hipStream_t>(stream);
     AtFwd f;
     f.s = at_shape(a, m);

@@ -110,6 +110,20 @@ def test_attention_refusals(L):
     assert attend(L, shape(B=0)) == m.OK and attend(L, shape(Nq=0)) == m.OK and attend_bwd(L, shape(B=0)) == m.OK and attend_bwd(L, shape(Nq=0, Nk=0)) == m.OK
 
 
+def test_results_in_an_operands_place_are_refused(L):
+    a, ws = shape(), 64 * P
+    far = {n: k * P for k, n in enumerate(("q", "k", "v", "o", "do"), 2)}
+    for n in ("q", "k", "v"):
+        assert attend(L, a, **{x: view(far[x]) for x in ("q", "k", "v")}, o=out(far[n]), ws=ws) == m.ERR_INVALID_ARG, n
+    res = dict(dq=out(10 * P), dk=out(11 * P), dv=out(12 * P))
+    for r in res:
+        for n in far:
+            assert attend_bwd(L, a, **{x: view(far[x]) for x in far}, **dict(res, **{r: out(far[n])}), ws=ws) == m.ERR_INVALID_ARG, (r, n)
+        for n in res:
+            if n != r:
+                assert attend_bwd(L, a, **{x: view(far[x]) for x in far}, **dict(res, **{r: res[n]}), ws=ws) == m.ERR_INVALID_ARG, (r, n)
+
+
 def test_bounds_refusals(L):
     f = lambda lo=P, hi=2 * P, B=2, Nq=5, Nk=7, w=0, kv=None, doc=None: L.mesa_attention_bounds(lo, hi, B, Nq, Nk, 1, w, kv, None, None, doc, None)  # noqa: E731
     bad, no = m.ERR_INVALID_ARG, m.ERR_UNSUPPORTED
