@@ -11,7 +11,7 @@
 // forms them once per tile into LDS -- angle and reduction in binary64, as positions times frequencies have more than 24
 // bits -- and all heads read them there.
 // Measured, 32768 tokens of 32 + 8 + 8 heads of 128, bfloat16 (a copy of as many bytes runs at 5.0 TB/s): forward 196 us (939 MB, 4.8 TB/s),
-// queries and keys again 109 us (503 MB, 4.6 TB/s), backward 174 us (839 MB, 4.8 TB/s).  One token of 24 heads of 64: 4.5 us.
+// queries and keys again 109 us (503 MB, 4.6 TB/s), backward 171 us (839 MB, 4.9 TB/s).  One token of 24 heads of 64: 4.5 us.
 #include <hip/hip_runtime.h>
 
 #include "api_util.hpp"
@@ -479,21 +479,14 @@ __global__ __launch_bounds__(kThreads, 4) void k_qkv_bwd(QkvGeom g, const int8_t
         }
     }
     if (!NORM) return;
-    // lanes that hold the same elements of different heads, then the four waves, each in a fixed order
-    float *sum = sums + 2 * kThreads * 8;                // [wave][2][8 * lph]
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            float v = (c ? mine_k : mine_q)[k];
-            for (uint32_t m = w.lph; m < 64; m <<= 1) v += __shfl_xor(v, int(m), 64);
-            if (w.sub == 0) sum[((w.wave * 2 + c) << (g.lph_log2 + 3)) + d0 + k] = v;
-        }
+    // threads that hold the same elements of different heads, in their order (exchanges between lanes before that took 3 us more)
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < 2 * g.D; i += kThreads) {
         const uint32_t c = i >= g.D, d = i - c * g.D;
+        const float *p = sums + c * (kThreads * 8) + d;
         float v = 0.0f;
-        for (uint32_t k = 0; k < kThreads / 64; ++k) v += sum[((k * 2 + c) << (g.lph_log2 + 3)) + d];
+#pragma unroll 8
+        for (uint32_t k = 0; k < kThreads; k += w.lph) v += p[k * 8];
         if (gridDim.x > 1) part[int64_t(blockIdx.x) * 2 * g.D + i] = v;
         else (c ? dgamma_k : dgamma_q)[d] = v;
     }
@@ -540,7 +533,7 @@ static size_t qkv_lds_fwd(const QkvGeom &g, bool again)
 }
 static size_t qkv_lds_bwd(const QkvGeom &g, bool norm)
 {
-    return (size_t(norm ? qkv_even(g.Hn) + g.D : 0) + g.tile * g.angles) * sizeof(float2) + (norm ? 2 * kThreads * 32 + size_t(8) * (8u << g.lph_log2) * 4 : 0);
+    return (size_t(norm ? qkv_even(g.Hn) + g.D : 0) + g.tile * g.angles) * sizeof(float2) + (norm ? 2 * kThreads * 32 : 0);
 }
 
 }  // namespace mesa
