@@ -230,6 +230,28 @@ __device__ __forceinline__ int ab_exponent(float bound)
 }
 __device__ __forceinline__ float ab_pow2(int e) { return __uint_as_float(uint32_t(127 + e) << 23); }   // -126 <= e <= 127
 
+// A wave's 32 result rows of accumulators (columns), by way of its own 32 * DP * 2 bytes of LDS: whole lines leave in 16-byte pieces, not eight bytes
+// a row (32 x 12 heads of 512 keys 168 -> 161 us).  row(i): where row i goes, null where there is none.
+template <typename T, int DP, typename Row> __device__ __forceinline__ void ab_put(char *lds, const at_acc *x, float mul, int lane, int D, Row row)
+{
+    constexpr int kPieces = DP / 8;
+    char *own = lds + (lane & 31) * (DP * 2) + (lane >> 5) * 8;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) at_store4<T>(own + (((d * 4 + w) ^ (lane & 7)) << 4), x[d][4 * w] * mul, x[d][4 * w + 1] * mul, x[d][4 * w + 2] * mul, x[d][4 * w + 3] * mul);
+    __builtin_amdgcn_wave_barrier();
+    const int piece = lane % kPieces;
+#pragma unroll
+    for (int k = 0; k < kPieces / 2; ++k) {
+        const int i = k * (64 / kPieces) + lane / kPieces;
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(lds + i * (DP * 2) + ((piece ^ (i & 7)) << 4));
+        char *p = row(i);
+        if (p && piece * 8 < D) *reinterpret_cast<u32x4 *>(p + piece * 16) = v;
+    }
+    __builtin_amdgcn_wave_barrier();
+}
+
 // scores of one accumulator in powers of two and, with a cap, the cap's derivative; away: place - key for register 0
 // ALONG: the registers count keys (a lane is a row), else rows (a lane is a key)
 template <bool CAP> __device__ __forceinline__ float ab_score(const AtShape &s, float x, float &slope)
@@ -402,15 +424,13 @@ template <typename T, int DP, int NW, int BN, bool CAP, bool BIAS, bool FINE> __
         if (j0 + BN <= wlo || j0 >= whi) continue;
         work(cur, j0, j0 >= flo && j0 + BN <= fhi);
     }
-    if (r_own >= s.R) return;
-    char *p = a.dq.p + int64_t(b) * a.dq.batch + int64_t(row.token) * a.dq.token + int64_t(hq) * a.dq.head;
-#pragma unroll
-    for (int d = 0; d < kDt; ++d)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const int e = d * 32 + 8 * w + 4 * half;
-            if (e < s.D) at_store4<T>(p + e * 2, dq[d][4 * w] * undo, dq[d][4 * w + 1] * undo, dq[d][4 * w + 2] * undo, dq[d][4 * w + 3] * undo);
-        }
+    __syncthreads();                                // the last tiles are done with
+    const uint32_t r0 = (rb * NW + wave) * 32;
+    char *out = a.dq.p + int64_t(b) * a.dq.batch + int64_t(hk) * s.G * a.dq.head;
+    ab_put<T, DP>(lds + wave * 32 * DP * 2, dq, undo, lane, s.D, [&](int i) __attribute__((always_inline)) -> char * {
+        const AtRow w = at_row(s, r0 + i);
+        return r0 + i < s.R ? out + int64_t(w.token) * a.dq.token + int64_t(w.g) * a.dq.head : nullptr;
+    });
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -691,8 +711,8 @@ template <typename T, int DP, bool CAP, bool BIAS, bool FINE> __device__ __force
         if (t & 2) work(at + 2 * kTile, info[cur][1], t >> 3 & 1, false, 0, nullptr);
         t = after;
     }
-    if (j_own >= s.Nk) return;
     if (a.part) {
+        if (j_own >= s.Nk) return;
         float *p = a.part + ((int64_t(split) * a.heads + head) * s.Nk + j_own) * 2 * s.D;
 #pragma unroll
         for (int d = 0; d < kDt; ++d)
@@ -706,18 +726,12 @@ template <typename T, int DP, bool CAP, bool BIAS, bool FINE> __device__ __force
             }
         return;
     }
-    char *pk = a.dk.p + int64_t(b) * a.dk.batch + int64_t(j_own) * a.dk.token + int64_t(hk) * a.dk.head;
-    char *pv = a.dv.p + int64_t(b) * a.dv.batch + int64_t(j_own) * a.dv.token + int64_t(hk) * a.dv.head;
-#pragma unroll
-    for (int d = 0; d < kDt; ++d)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const int e = d * 32 + 8 * w + 4 * half;
-            if (e < s.D) {
-                at_store4<T>(pk + e * 2, dk[d][4 * w] * undo, dk[d][4 * w + 1] * undo, dk[d][4 * w + 2] * undo, dk[d][4 * w + 3] * undo);
-                at_store4<T>(pv + e * 2, dv[d][4 * w] * undo_v, dv[d][4 * w + 1] * undo_v, dv[d][4 * w + 2] * undo_v, dv[d][4 * w + 3] * undo_v);
-            }
-        }
+    __syncthreads();                                // the last tiles are done with
+    char *pk = a.dk.p + int64_t(b) * a.dk.batch + int64_t(j0) * a.dk.token + int64_t(hk) * a.dk.head;
+    char *pv = a.dv.p + int64_t(b) * a.dv.batch + int64_t(j0) * a.dv.token + int64_t(hk) * a.dv.head;
+    char *mid = lds + wave * 32 * DP * 2;
+    ab_put<T, DP>(mid, dk, undo, lane, s.D, [&](int i) __attribute__((always_inline)) { return j0 + i < s.Nk ? pk + int64_t(i) * a.dk.token : nullptr; });
+    ab_put<T, DP>(mid, dv, undo_v, lane, s.D, [&](int i) __attribute__((always_inline)) { return j0 + i < s.Nk ? pv + int64_t(i) * a.dv.token : nullptr; });
 }
 
 // Up to 64 elements a wave of either walk fits two to a SIMD, so that one launch can have both: the rows' workgroups fill in where the
