@@ -64,7 +64,8 @@ struct AtBwd {
     AbRows w;
     AbOrder order;
     float *part;                       // [split][b * Hk + head][Nk][2][D]; null: no split
-    uint32_t heads, key_blocks, splits, row_blocks;
+    float *part_q;                     // [row split][b * Hk + head][row][D]; null: no split
+    uint32_t heads, key_blocks, splits, row_blocks, row_splits;
 };
 
 // codes to contiguous (B, heads, tokens, D) elements, as mesa_dequantize; eight per thread
@@ -275,7 +276,7 @@ template <typename T, int DP, int NW, int BN, bool CAP, bool BIAS, bool FINE> __
     __shared__ uint64_t seen[NW];
     const AtShape &s = a.s;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), half = lane >> 5;
-    const uint32_t head = block % a.heads, rb = a.row_blocks - 1 - block / a.heads;
+    const uint32_t head = block % a.heads, rest = block / a.heads, split = rest % a.row_splits, rb = a.row_blocks - 1 - rest / a.row_splits;
     const int b = int(head / uint32_t(s.Hk)), hk = int(head) - b * s.Hk;
     const uint32_t r_own = (rb * NW + wave) * 32 + (lane & 31), r = r_own < s.R ? r_own : s.R - 1;
     const AtRow row = at_row(s, r);
@@ -312,7 +313,14 @@ template <typename T, int DP, int NW, int BN, bool CAP, bool BIAS, bool FINE> __
         full_lo[w] = __builtin_amdgcn_readfirstlane(range[2][w]);
         full_hi[w] = __builtin_amdgcn_readfirstlane(range[3][w]);
     }
-    const int t0 = __builtin_amdgcn_readfirstlane(bhi > 0 ? blo / BN : 0), t1 = __builtin_amdgcn_readfirstlane(bhi > 0 ? (bhi + BN - 1) / BN : 0);
+    int t0 = bhi > 0 ? blo / BN : 0, t1 = bhi > 0 ? (bhi + BN - 1) / BN : 0;
+    if (a.row_splits > 1) {
+        const int per = (t1 - t0 + int(a.row_splits) - 1) / int(a.row_splits);
+        t0 += int(split) * per;
+        t1 = t0 + per < t1 ? t0 + per : t1;
+    }
+    t0 = __builtin_amdgcn_readfirstlane(t0);
+    t1 = __builtin_amdgcn_readfirstlane(t1);
 
     const char *kbase = a.k.p + int64_t(b) * a.k.batch + int64_t(hk) * a.k.head, *vbase = a.v.p + int64_t(b) * a.v.batch + int64_t(hk) * a.v.head;
     Tile tk, tv;
@@ -423,6 +431,18 @@ template <typename T, int DP, int NW, int BN, bool CAP, bool BIAS, bool FINE> __
         if (t + 1 < t1) fetch(t + 1);
         if (j0 + BN <= wlo || j0 >= whi) continue;
         work(cur, j0, j0 >= flo && j0 + BN <= fhi);
+    }
+    if (a.part_q) {
+        if (r_own >= s.R) return;
+        float *p = a.part_q + ((int64_t(split) * a.heads + head) * s.R + r_own) * s.D;
+#pragma unroll
+        for (int d = 0; d < kDt; ++d)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int e = d * 32 + 8 * w + 4 * half;
+                if (e < s.D) *reinterpret_cast<float4 *>(p + e) = make_float4(dq[d][4 * w] * undo, dq[d][4 * w + 1] * undo, dq[d][4 * w + 2] * undo, dq[d][4 * w + 3] * undo);
+            }
+        return;
     }
     __syncthreads();                                // the last tiles are done with
     const uint32_t r0 = (rb * NW + wave) * 32;
@@ -734,15 +754,15 @@ template <typename T, int DP, bool CAP, bool BIAS, bool FINE> __device__ __force
     ab_put<T, DP>(mid, dv, undo_v, lane, s.D, [&](int i) __attribute__((always_inline)) { return j0 + i < s.Nk ? pv + int64_t(i) * a.dv.token : nullptr; });
 }
 
-// Up to 64 elements a wave of either walk fits two to a SIMD, so that one launch can have both: the rows' workgroups fill in where the
-// keys' run out (8 x 12 heads of 197 keys 23.6 -> 15.1 us, 32 x 12 46.2 -> 44.1).  With many workgroups there is nothing to fill in, and dq
-// alone has more waves (4 x 4 heads of 4001 keys: 390 us in two launches, 402 in one).
-template <typename T, bool CAP, bool BIAS, bool FINE>
-__global__ __launch_bounds__(256, 2) void k_attn_both(const AtBwd a)
+// Both walks in one launch: the rows' workgroups fill in where the keys' run out (8 x 12 heads of 197 keys 23.6 -> 15.1 us, 32 x 12 46.2 ->
+// 44.1).  With many workgroups there is nothing to fill in, and dq alone has more waves (4 x 4 heads of 4001 keys: 390 us in two launches,
+// 402 in one).  Tiles of 64 keys for dq here, whose waves are few and wait for them (2 x 12 heads of 4096 keys 405 -> 395 us; 8 x 12 of 197 15.0 -> 15.4).
+template <typename T, int DP, bool CAP, bool BIAS, bool FINE>
+__global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_both(const AtBwd a)
 {
     const uint32_t keys = a.heads * a.key_blocks * a.splits;
-    if (blockIdx.x < keys) ab_dkv<T, 64, CAP, BIAS, FINE>(a, blockIdx.x);
-    else ab_dq<T, 64, 4, 32, CAP, BIAS, FINE>(a, blockIdx.x - keys);
+    if (blockIdx.x < keys) ab_dkv<T, DP, CAP, BIAS, FINE>(a, blockIdx.x);
+    else ab_dq<T, DP, 4, 64, CAP, BIAS, FINE>(a, blockIdx.x - keys);
 }
 template <typename T, int DP, bool CAP, bool BIAS, bool FINE>
 __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_dkv(const AtBwd a)
@@ -755,29 +775,43 @@ __global__ __launch_bounds__(256, 2) void k_attn_dq(const AtBwd a)
     ab_dq<T, DP, 4, 32, CAP, BIAS, FINE>(a, blockIdx.x);
 }
 
-// the splits added up in their order, four elements of dk or dv per thread
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_attn_add(const AtBwd a, int64_t pieces)
+// the splits added up in their order, four elements per thread: of dk or dv, behind those of dq
+__device__ __forceinline__ float4 ab_sum(const float *p, int64_t step, uint32_t splits)
 {
-    const AtShape &s = a.s;
-    const int64_t id = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-    if (id >= pieces) return;
-    const int quads = s.D / 2;                              // of a key: D/4 of dk, D/4 of dv
-    const int64_t at = id / quads, head = at / s.Nk, step = int64_t(a.heads) * s.Nk * 2 * s.D;
-    const int x = int(id - at * quads), j = int(at - head * s.Nk);
-    const float *p = a.part + at * 2 * s.D + x * 4;
     float4 v = *reinterpret_cast<const float4 *>(p);
-    for (uint32_t k = 1; k < a.splits; ++k) {
+    for (uint32_t k = 1; k < splits; ++k) {
         const float4 u = *reinterpret_cast<const float4 *>(p + k * step);
         v.x += u.x;
         v.y += u.y;
         v.z += u.z;
         v.w += u.w;
     }
-    const int b = int(head) / s.Hk, hk = int(head) - b * s.Hk;
-    const bool key = x < s.D / 4;
-    const AtOut &o = key ? a.dk : a.dv;
-    at_store4<T>(o.p + int64_t(b) * o.batch + int64_t(j) * o.token + int64_t(hk) * o.head + (key ? x : x - s.D / 4) * 8, v.x, v.y, v.z, v.w);
+    return v;
+}
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_attn_add(const AtBwd a, int64_t pieces, int64_t row_pieces)
+{
+    const AtShape &s = a.s;
+    int64_t id = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+    if (id < pieces) {
+        const int quads = s.D / 2;                              // of a key: D/4 of dk, D/4 of dv
+        const int64_t at = id / quads, head = at / s.Nk;
+        const int x = int(id - at * quads), j = int(at - head * s.Nk);
+        const float4 v = ab_sum(a.part + at * 2 * s.D + x * 4, int64_t(a.heads) * s.Nk * 2 * s.D, a.splits);
+        const int b = int(head) / s.Hk, hk = int(head) - b * s.Hk;
+        const bool key = x < s.D / 4;
+        const AtOut &o = key ? a.dk : a.dv;
+        at_store4<T>(o.p + int64_t(b) * o.batch + int64_t(j) * o.token + int64_t(hk) * o.head + (key ? x : x - s.D / 4) * 8, v.x, v.y, v.z, v.w);
+        return;
+    }
+    id -= pieces;
+    if (id >= row_pieces) return;
+    const int quads = s.D / 4;
+    const int64_t at = id / quads, head = at / s.R;
+    const int x = int(id - at * quads), b = int(head) / s.Hk, hk = int(head) - b * s.Hk;
+    const AtRow row = at_row(s, uint32_t(at - head * s.R));
+    const float4 v = ab_sum(a.part_q + at * s.D + x * 4, int64_t(a.heads) * s.R * s.D, a.row_splits);
+    at_store4<T>(a.dq.p + int64_t(b) * a.dq.batch + int64_t(row.token) * a.dq.token + int64_t(hk * s.G + int(row.g)) * a.dq.head + x * 8, v.x, v.y, v.z, v.w);
 }
 
 // zeros: dq where there are no keys, dk and dv where there are no queries
@@ -793,8 +827,8 @@ __global__ __launch_bounds__(kThreads) void k_attn_zero(AtOut o, int heads, int 
 
 struct AtBwdPlan {
     AbOrder order;
-    uint32_t blocks, key_blocks, splits, row_blocks;
-    size_t info, part, operand[3], total;       // bytes
+    uint32_t blocks, key_blocks, splits, row_blocks, row_splits;
+    size_t info, part, part_q, operand[3], total;       // bytes
 };
 static size_t ab_up(size_t n) { return (n + 255) & ~size_t(255); }
 static AtBwdPlan at_bwd_plan(const mesa_attention &a, const bool codes[3])
@@ -815,15 +849,26 @@ static AtBwdPlan at_bwd_plan(const mesa_attention &a, const bool codes[3])
     p.row_blocks = uint32_t(ceil_div(R, 128));
     // few keys and long walks: the rows' tiles are dealt out to several workgroups and their sums added up
     const int64_t have = heads * p.key_blocks, most = o.tiles / 16;
-    int64_t n = have > 0 ? 1024 / have : 1;
+    int64_t n = have > 0 ? 1024 / have : 1, m = 1;
     n = n > most ? most : n;
+    // So few workgroups of either walk that compute units have nothing to do, and walks long enough to pay for the addition's launch (4 us): both
+    // are dealt out, down to four tiles of rows or 192 keys each.  Two heads of 64, causal: 911 keys 32 -> 23 us, 2000 60 -> 33, 4000 111 -> 46;
+    // of 128, 4000 keys 187 -> 90; where a window leaves nothing to deal out, 20 -> 21.5.
+    const int64_t rows = heads * p.row_blocks;
+    if (have > 0 && have + rows <= 512 && o.tiles >= 24 && a.Nk >= 768) {
+        const int64_t few = 256 / have < o.tiles / 4 ? 256 / have : o.tiles / 4;
+        n = n > few ? n : few;
+        m = 512 / rows < a.Nk / 192 ? 512 / rows : a.Nk / 192;
+    }
     n = n > 32 ? 32 : n < 1 ? 1 : n;
     p.splits = uint32_t(n);
+    p.row_splits = uint32_t(m > 8 ? 8 : m);
     const size_t h = size_t(heads);
     p.info = ab_up(h * o.tiles * kAbWords * 128) + ab_up(h * o.tiles * sizeof(int4)) + ab_up(h * p.blocks * sizeof(float2)) + ab_up(h * p.key_blocks * sizeof(float));
     p.part = n > 1 ? ab_up(size_t(n) * h * size_t(a.Nk) * 2 * size_t(a.D) * sizeof(float)) : 0;
+    p.part_q = p.row_splits > 1 ? ab_up(size_t(p.row_splits) * h * size_t(R) * size_t(a.D) * sizeof(float)) : 0;
     const int64_t tokens[3] = {a.Nq, a.Nk, a.Nk}, hs[3] = {a.Hq, a.Hk, a.Hk};
-    p.total = p.info + p.part;
+    p.total = p.info + p.part + p.part_q;
     for (int k = 0; k < 3; ++k) {
         p.operand[k] = codes[k] ? ab_up(size_t(a.B) * size_t(tokens[k]) * size_t(hs[k]) * size_t(a.D) * 2) : 0;
         p.total += p.operand[k];
@@ -833,18 +878,18 @@ static AtBwdPlan at_bwd_plan(const mesa_attention &a, const bool codes[3])
 
 template <typename T, int DP, bool CAP, bool BIAS, bool FINE> static mesa_status at_bwd_launch(const AtBwd &a, hipStream_t s)
 {
-    const uint32_t keys = a.heads * a.key_blocks * a.splits, rows = a.heads * a.row_blocks;
-    const bool both = DP == 64 && keys < 1024;         // two rounds of workgroups
-    if (both) hipLaunchKernelGGL((k_attn_both<T, CAP, BIAS, FINE>), dim3(keys + rows), dim3(256), 0, s, a);
+    const uint32_t keys = a.heads * a.key_blocks * a.splits, rows = a.heads * a.row_blocks * a.row_splits;
+    const bool both = DP == 64 ? keys < 1024 : keys + rows <= 256;      // two rounds of workgroups; one to a compute unit
+    if (both) hipLaunchKernelGGL((k_attn_both<T, DP, CAP, BIAS, FINE>), dim3(keys + rows), dim3(256), 0, s, a);
     else hipLaunchKernelGGL((k_attn_dkv<T, DP, CAP, BIAS, FINE>), dim3(keys), dim3(256), 0, s, a);
     if (const mesa_status st = launch_status()) return st;
-    if (a.splits > 1) {
-        const int64_t pieces = int64_t(a.heads) * a.s.Nk * (a.s.D / 2);
-        hipLaunchKernelGGL(k_attn_add<T>, dim3(uint32_t(ceil_div(pieces, kThreads))), dim3(kThreads), 0, s, a, pieces);
+    if (!both) {
+        hipLaunchKernelGGL((k_attn_dq<T, DP, CAP, BIAS, FINE>), dim3(rows), dim3(256), 0, s, a);
         if (const mesa_status st = launch_status()) return st;
     }
-    if (both) return MESA_OK;
-    hipLaunchKernelGGL((k_attn_dq<T, DP, CAP, BIAS, FINE>), dim3(rows), dim3(256), 0, s, a);
+    const int64_t pieces = a.splits > 1 ? int64_t(a.heads) * a.s.Nk * (a.s.D / 2) : 0, row_pieces = a.row_splits > 1 ? int64_t(a.heads) * a.s.R * (a.s.D / 4) : 0;
+    if (pieces + row_pieces == 0) return MESA_OK;
+    hipLaunchKernelGGL(k_attn_add<T>, dim3(uint32_t(ceil_div(pieces + row_pieces, kThreads))), dim3(kThreads), 0, s, a, pieces, row_pieces);
     return launch_status();
 }
 // Up to kAbFine keys the call is bound by what it reads and writes (14 products of 64 keys to a row's four vectors), and with so few terms to
@@ -881,7 +926,7 @@ static mesa_status at_bwd(const mesa_attention &m, AtBwd &a, const AtBwdPlan &p,
     }
     AtView *view[3] = {&a.q, &a.k, &a.v};
     const int64_t tokens[3] = {m.Nq, m.Nk, m.Nk}, heads[3] = {m.Hq, m.Hk, m.Hk};
-    char *out = ws + p.info + p.part;
+    char *out = ws + p.info + p.part + p.part_q;
     AbOperands ops;
     ops.count = 0;
     ops.values = false;
@@ -976,6 +1021,7 @@ extern "C" MESA_EXPORT mesa_status mesa_attention_bwd_q(mesa_attention a, mesa_a
     f.key_blocks = p.key_blocks;
     f.splits = p.splits;
     f.row_blocks = p.row_blocks;
+    f.row_splits = p.row_splits;
     char *w = static_cast<char *>(ws);
     const size_t h = size_t(heads), tiles_at = ab_up(h * p.order.tiles * kAbWords * 128), most_at = tiles_at + ab_up(h * p.order.tiles * sizeof(int4));
     f.order = p.order;
@@ -986,6 +1032,7 @@ extern "C" MESA_EXPORT mesa_status mesa_attention_bwd_q(mesa_attention a, mesa_a
     f.w.blocks = p.blocks;
     f.w.key_blocks = p.key_blocks;
     f.part = p.splits > 1 ? reinterpret_cast<float *>(w + p.info) : nullptr;
+    f.part_q = p.row_splits > 1 ? reinterpret_cast<float *>(w + p.info + p.part) : nullptr;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool bias = m.slopes != nullptr;
     return dt == MESA_F16 ? at_bwd<_Float16>(a, f, p, in, codes, w, bias, s) : at_bwd<__bf16>(a, f, p, in, codes, w, bias, s);

@@ -113,6 +113,11 @@ CASES = [  # B, Nq, Nk, Hq, Hk, D, mask, cap, bias, layout
     # capped scores over many keys
     (1, 530, 530, 4, 2, 72, dict(causal=True, prefix=True), 15.0, True, "packed"),
     (1, 150, 700, 2, 1, 64, dict(causal=True, window=90), 30.0, False, "bnhd"),
+    # few workgroups and long walks: keys and rows are dealt out in the backward
+    (1, 911, 911, 2, 2, 96, dict(causal=True), 30.0, True, "packed"),
+    (2, 801, 1001, 3, 1, 64, dict(causal=True, docs=3, pad=True), 0, False, "bhnd"),
+    (1, 800, 790, 2, 1, 128, dict(window=50), 0, True, "bnhd"),
+    (1, 60, 900, 16, 1, 40, {}, 0, False, "bnhd"),
 ]
 FEW = [  # few rows over many keys: the keys are shared out
     (1, 1, 5000, 8, 1, 128, dict(causal=True), 0, False, "bnhd"),
