@@ -356,25 +356,29 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 && !BIAS ? 4 : 2) v
         }
 }
 
-// The splits of a row joined, with weights 2^(lse_s - max): a workgroup per row, eight groups of 32 threads with four elements each
-// share out the splits and meet in LDS.
-template <typename T>
+// The splits of a row joined, with weights 2^(lse_s - max): 32 threads with four elements each.  FEW: a workgroup per row, whose eight such groups
+// share out the splits and meet in LDS; else a row to each of
+// them, or to 16 threads up to 64 elements (32768 rows of four splits 24.7 -> 7.5 us).
+template <typename T, bool FEW>
 __global__ __launch_bounds__(kThreads) void k_attn_join(const AtFwd a)
 {
     constexpr int kU = 4, kGroups = kThreads / 32;
+    static_assert(kThreads == 256, "8 - log2 rows of a workgroup");
     const AtShape &s = a.s;
-    __shared__ float sums[kGroups][32][5];
-    __shared__ float tops[kGroups];
-    const int64_t at = blockIdx.x, step = int64_t(a.heads) * s.R;     // (b, key head, row)
-    const int quad = threadIdx.x & 31, group = threadIdx.x >> 5, e = quad * 4;
+    __shared__ float sums[FEW ? kGroups : 1][32][5];
+    __shared__ float tops[FEW ? kGroups : 1];
+    const int log2 = FEW || s.D > 64 ? 5 : 4, quad = threadIdx.x & ((1 << log2) - 1), group = threadIdx.x >> log2, e = quad * 4;
+    const int64_t step = int64_t(a.heads) * s.R, at = FEW ? int64_t(blockIdx.x) : (int64_t(blockIdx.x) << (8 - log2)) + group;     // (b, key head, row)
+    if (!FEW && at >= step) return;
+    const int first = FEW ? group : 0, stride = FEW ? kGroups : 1;
     const bool act = e < s.D;
     float top = kAtLow, total = 0.0f, x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k0 = group; k0 < int(a.splits); k0 += kGroups * kU) {
+    for (int k0 = first; k0 < int(a.splits); k0 += stride * kU) {
         float z[kU];
         float4 v[kU];
 #pragma unroll
         for (int u = 0; u < kU; ++u) {                                // four requested together; behind the last one this group's first again, without weight
-            const int64_t k = (k0 + u * kGroups < int(a.splits) ? k0 + u * kGroups : k0) * step + at;
+            const int64_t k = (k0 + u * stride < int(a.splits) ? k0 + u * stride : k0) * step + at;
             z[u] = a.part_lse[k];
             v[u] = act ? *reinterpret_cast<const float4 *>(a.part_o + k * s.D + e) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
@@ -388,7 +392,7 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(const AtFwd a)
         for (int k = 0; k < 4; ++k) x[k] *= f;
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
-            const float w = k0 + u * kGroups < int(a.splits) ? at_exp2(z[u] - m) : 0.0f;      // a split that saw nothing: -infinity, no weight
+            const float w = k0 + u * stride < int(a.splits) ? at_exp2(z[u] - m) : 0.0f;      // a split that saw nothing: -infinity, no weight
             total += w;
             x[0] = fmaf(w, v[u].x, x[0]);
             x[1] = fmaf(w, v[u].y, x[1]);
@@ -396,23 +400,27 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(const AtFwd a)
             x[3] = fmaf(w, v[u].w, x[3]);
         }
     }
-    if (quad == 0) tops[group] = top;
+    float m = top;
+    if (FEW) {
+        if (quad == 0) tops[group] = top;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) sums[group][quad][k] = x[k];
-    sums[group][quad][4] = total;
-    __syncthreads();
-    if (group > 0 || !act) return;
-    float m = kAtLow;
+        for (int k = 0; k < 4; ++k) sums[group][quad][k] = x[k];
+        sums[group][quad][4] = total;
+        __syncthreads();
+        if (group > 0) return;
+        m = kAtLow;
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) m = fmaxf(m, tops[g]);
-    total = x[0] = x[1] = x[2] = x[3] = 0.0f;
+        for (int g = 0; g < kGroups; ++g) m = fmaxf(m, tops[g]);
+        total = x[0] = x[1] = x[2] = x[3] = 0.0f;
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-        const float w = at_exp2(tops[g] - m);
-        total = fmaf(w, sums[g][quad][4], total);
+        for (int g = 0; g < kGroups; ++g) {
+            const float w = at_exp2(tops[g] - m);
+            total = fmaf(w, sums[g][quad][4], total);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = fmaf(w, sums[g][quad][k], x[k]);
+            for (int k = 0; k < 4; ++k) x[k] = fmaf(w, sums[g][quad][k], x[k]);
+        }
     }
+    if (!act) return;
     const float inv = total == 0.0f ? 0.0f : 1.0f / total;
     const uint32_t head = uint32_t(at / s.R), r = uint32_t(at - int64_t(head) * s.R);
     const int b = int(head) / s.Hk, hk = int(head) - b * s.Hk;
@@ -438,9 +446,12 @@ static AtFwdPlan at_fwd_plan(const mesa_attention &a)
     p.row_blocks = uint32_t(ceil_div(R, p.waves * 32));
     // One wave per SIMD fits the wide heads' registers: 1024 workgroups at a time.  Two rounds of them even out lengths that differ (16 x 4
     // heads over 16381 keys or fewer: 24 splits 90 us, 32 85, 64 88); with less than 256 keys each the rounds' own cost takes more
-    // than that (3001 keys: 23 splits 21.7 us, 16 17.5).
-    const int64_t have = heads * p.row_blocks, most = a.Nk / (p.waves == 1 ? 128 : 512);
-    int64_t n = have > 0 ? (p.waves == 1 ? 2048 : 384) / have : 1;
+    // than that (3001 keys: 23 splits 21.7 us, 16 17.5).  Of four waves, one round as registers have it, four workgroups to a compute unit up to
+    // 64 elements and two above (8 heads of 4096 tokens 67 -> 41 us and 103 -> 70; 16 x 64 tokens after 16381 376 -> 296); down to 192 keys
+    // where workgroups are few (2 heads of 911 tokens 19 -> 12.5, 8 of 800 18 -> 14.5), 512 where the join's rows are many (8 key heads of 4 x
+    // 1000 rows: 21 us whole, 29 in splits of 250).
+    const int64_t have = heads * p.row_blocks, most = a.Nk / (p.waves == 1 ? 128 : have <= 64 ? 192 : 512);
+    int64_t n = have > 0 ? (p.waves == 1 ? 2048 : a.D > 64 ? 512 : 1024) / have : 1;
     if (p.waves == 1 && n * 256 > a.Nk) n = 1024 / have;
     n = n > most ? most : n;
     n = n > 128 ? 128 : n < 1 ? 1 : n;
@@ -554,8 +565,11 @@ extern "C" MESA_EXPORT mesa_status mesa_attention_fwd(mesa_attention a, mesa_att
     else a.D <= 64 ? at_fwd_forms<__bf16, 64>(f, p, cap, bias, s) : at_fwd_forms<__bf16, 128>(f, p, cap, bias, s);
     if (const mesa_status st = launch_status()) return st;
     if (p.splits > 1) {
-        if (half) hipLaunchKernelGGL(k_attn_join<_Float16>, dim3(uint32_t(groups * f.s.R)), dim3(kThreads), 0, s, f);
-        else hipLaunchKernelGGL(k_attn_join<__bf16>, dim3(uint32_t(groups * f.s.R)), dim3(kThreads), 0, s, f);
+        const int64_t rows = groups * f.s.R;
+        const bool few = p.splits > 8 && rows <= 4096;
+        const dim3 grid(uint32_t(few ? rows : ceil_div(rows, a.D > 64 ? 8 : 16)));
+        auto *join = half ? (few ? k_attn_join<_Float16, true> : k_attn_join<_Float16, false>) : (few ? k_attn_join<__bf16, true> : k_attn_join<__bf16, false>);
+        hipLaunchKernelGGL(join, grid, dim3(kThreads), 0, s, f);
         return launch_status();
     }
     return MESA_OK;

@@ -125,6 +125,8 @@ FEW = [  # few rows over many keys: the keys are shared out
     (1, 5, 3000, 12, 2, 80, dict(causal=True, docs=3), 0, True, "bnhd"),
     (1, 64, 4100, 4, 1, 128, dict(causal=True), 0, False, "bnhd"),
     (2, 33, 2050, 2, 1, 64, dict(window=300), 0, False, "bnhd"),
+    (1, 600, 2100, 10, 2, 40, dict(causal=True), 30.0, False, "bnhd"),   # many rows to a join of few splits, and of many
+    (1, 131, 2500, 33, 1, 80, dict(causal=True, docs=4), 0, True, "bhnd"),
 ]
 
 
