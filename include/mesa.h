@@ -449,7 +449,8 @@ mesa_status mesa_qkv_norm_rope_bwd_q(const int8_t *q, mesa_qkv_heads h, const vo
  * p = q_start[b] + i (q_start NULL: Nk - Nq + i) among that sequence's kv_len[b] keys (NULL: Nk; taken as at most Nk):
  *   hi = kv_len;  causal: hi = min(kv_len, max(p + 1, prefix[b]))         (prefix NULL: none)
  *   window > 0:   lo = p - window + 1;  not causal: hi = min(hi, p + window) too
- *   doc (B, Nk):  lo, hi within the run of keys with doc[b][p]'s number; numbers do not decrease along a row
+ *   doc (B, Nk):  lo, hi within the run of keys with doc[b][p]'s number; numbers do not decrease along a row's kv_len keys
+ *                 (what lies behind them is not looked at)
  * lo = hi = 0 for a query without a place (p < 0 or p >= kv_len) or one that sees nothing.  Every result has 0 <= lo <= hi <= Nk,
  * whatever the lists hold.
  * lo, hi: (B, Nq) int32 (out).  kv_len, q_start, prefix: [B] int32.  0 <= Nq, Nk < 2^30; B*Nq < 2^40; window >= 0.
@@ -467,7 +468,8 @@ mesa_status mesa_attention_bounds(int32_t *lo, int32_t *hi, int64_t B, int64_t N
  * sequence sees, and rows of q, o and do whose query sees nothing, does not matter (infinities and NaN neither).
  * Storage is binary16 or bfloat16; scores, softmax and sums are binary32, the probabilities that enter a product are rounded to dt.
  * 1 <= Hk, Hq a multiple of Hk; D a multiple of 8, 8 <= D <= 128, else MESA_ERR_UNSUPPORTED (MESA_F32 too).
- * Nq, Nk < 2^30, Nq * (Hq/Hk) < 2^31, Nq * D and Nk * D < 2^34, and what a launch can have of workgroups; scale > 0 and cap >= 0, finite.  Nk = 0: o = 0, lse = -infinity.
+ * Nq, Nk < 2^30, Nq * (Hq/Hk) < 2^31, Nq * D and Nk * D < 2^34, and what a launch can have of workgroups; scale > 0 and cap >= 0, scale and scale / cap
+ * below 1e37; cap <= 256, else MESA_ERR_UNSUPPORTED.  Nk = 0: o = 0, lse = -infinity.
  */
 typedef struct mesa_attention {
     int64_t B, Nq, Nk, Hq, Hk, D;

@@ -30,6 +30,7 @@ typedef __bf16 at_v2b __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr float kAtLow = -3.0e38f;      // a running maximum before anything is seen; finite, so that (-inf) - it is -inf
+constexpr float kAtMostCap = 256.0f;    // tanh is formed with an absolute error, 2^-23 or so, which a score has cap-fold
 constexpr int kAtDrop = 8;              // binary16 probabilities of the backward carry this power of two, clear of subnormal values
 
 template <typename T> struct AtNum;
@@ -264,13 +265,13 @@ inline bool at_valid(const mesa_attention &a)
 {
     const int64_t top = int64_t(1) << 30;
     return a.B >= 0 && a.Nq >= 0 && a.Nk >= 0 && a.Hk >= 1 && a.Hq >= 1 && a.Hq % a.Hk == 0 && a.D >= 1 && a.scale > 0.0f && a.scale < __builtin_inff() && a.cap >= 0.0f &&
-           a.cap < __builtin_inff() && a.B < top && a.Nq < top && a.Nk < top && a.Hq < top && a.Hk < top;
+           a.cap < __builtin_inff() && a.scale < 1.0e37f && (a.cap == 0.0f || a.scale / a.cap < 1.0e37f) && a.B < top && a.Nq < top && a.Nk < top && a.Hq < top && a.Hk < top;
 }
 // MESA_OK, or why the kernels do not take this shape
 inline mesa_status at_supported(const mesa_attention &a, mesa_dtype dt)
 {
     if (!valid_dtype(dt) || !at_valid(a)) return MESA_ERR_INVALID_ARG;
-    if (dt == MESA_F32 || a.D % 8 != 0 || a.D > 128) return MESA_ERR_UNSUPPORTED;
+    if (dt == MESA_F32 || a.D % 8 != 0 || a.D > 128 || a.cap > kAtMostCap) return MESA_ERR_UNSUPPORTED;
     // rows and pieces of a head are counted in 32 bits, workgroups by what a launch takes; below these, products of two sizes fit 64 bits
     const int64_t top = int64_t(1) << 31;
     if (a.Nq >= top / (a.Hq / a.Hk) || a.Nq >= top * 8 / a.D || a.Nk >= top * 8 / a.D || a.B > most_workgroups(256) / a.Hk) return MESA_ERR_UNSUPPORTED;

@@ -93,7 +93,7 @@ __global__ __launch_bounds__(kThreads) void k_attn_bounds(int32_t *__restrict__ 
             const int mine = d[first], at = at_search(0, first, lane, [&](int x) { return d[x] < mine; });
             if (lane == 0) end[0] = at;
         } else if (wave == 1) {
-            const int mine = d[last], at = at_search(last + 1, Nk, lane, [&](int x) { return d[x] <= mine; });
+            const int mine = d[last], at = at_search(last + 1, n, lane, [&](int x) { return d[x] <= mine; });
             if (lane == 0) end[1] = at;
         }
         __syncthreads();
@@ -160,9 +160,11 @@ struct AtFwd {
 // CAP: kAtCapped takes at_tanh<true>.  kAtCappedLong leaves r = -1 / (2^u + 1) in a score's place, u = 2 log2(e) s / cap, whose score is
 // cap + 2 cap r: both go into the exponent's one multiply-add, three instructions less of eleven a score where vector instructions are
 // what binds (2 x 8192 x 16 heads of 128 717 -> 670 us, of 64 486 -> 423).  Such a score is off by 2^-23 of the cap or so, whatever its
-// size; lse over 600 keys then by 1.3e-7 of itself (4e-8 with tanh), where a query sees one key of them by 1.5e-6: so only from kAtLong keys on.
+// size; lse over 600 keys then by 1.3e-7 of itself (4e-8 with tanh), where a query sees one key of them by 1.5e-6 (cap 30): so only from kAtLong keys on and for
+// caps up to kAtLongCap.
 enum { kAtUncapped = 0, kAtCapped, kAtCappedLong };
 constexpr int kAtLong = 512;
+constexpr float kAtLongCap = 64.0f;
 template <typename T, int DP, int NW, int BN, int CAP, bool BIAS>
 __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DP == 64 && !BIAS ? 4 : 2) void k_attn_fwd(const AtFwd a)
 {
@@ -468,7 +470,7 @@ template <typename T, int DP, bool CAP, bool BIAS> static void at_fwd_launch(con
     const dim3 grid(a.heads * a.row_blocks * a.splits);
     constexpr int kCap = CAP ? kAtCapped : kAtUncapped, kLong = CAP ? kAtCappedLong : kAtUncapped;
     if (p.waves == 1) hipLaunchKernelGGL((k_attn_fwd<T, DP, 1, 32, kCap, BIAS>), grid, dim3(64), 0, s, a);     // what it reads takes longer
-    else if (a.s.Nk < kAtLong) hipLaunchKernelGGL((k_attn_fwd<T, DP, 4, 64, kCap, BIAS>), grid, dim3(256), 0, s, a);
+    else if (a.s.Nk < kAtLong || a.s.cap2 > kAtLongCap * kLog2e) hipLaunchKernelGGL((k_attn_fwd<T, DP, 4, 64, kCap, BIAS>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((k_attn_fwd<T, DP, 4, 64, kLong, BIAS>), grid, dim3(256), 0, s, a);
 }
 template <typename T, int DP> static void at_fwd_forms(const AtFwd &a, const AtFwdPlan &p, bool cap, bool bias, hipStream_t s)

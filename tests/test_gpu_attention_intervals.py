@@ -46,6 +46,21 @@ def test_bounds(B, Nq, Nk, kw):
     assert torch.equal(lo.cpu(), wlo) and torch.equal(hi.cpu(), whi)
 
 
+def test_what_lies_behind_the_keys_is_not_looked_at():
+    """a padded batch whose padding carries a number of its own, below the documents'"""
+    B, N = 3, 5000
+    n = torch.tensor([4100, 700, 1], dtype=torch.int32)
+    doc = torch.cumsum((torch.rand(B, N, generator=torch.Generator().manual_seed(4)) < 0.002).int(), 1).int()
+    clean = doc.clone()
+    for b in range(B):
+        doc[b, n[b]:] = -100
+    lo, hi, wlo, whi = (torch.empty(B, N, dtype=torch.int32, device=DEV) for _ in range(4))
+    start = torch.zeros(B, dtype=torch.int32, device=DEV)
+    m.mesa_attention_bounds(lo, hi, N, False, kv_len=n.to(DEV), q_start=start, doc=doc.to(DEV))
+    m.mesa_attention_bounds(wlo, whi, N, False, kv_len=n.to(DEV), q_start=start, doc=clean.to(DEV))
+    assert torch.equal(lo, wlo) and torch.equal(hi, whi) and (hi[0, :4100] > lo[0, :4100]).all()
+
+
 def test_bounds_stay_within_the_keys_whatever_the_lists_hold():
     B, Nq, Nk = 6, 50, 40
     g = torch.Generator().manual_seed(1)
@@ -113,6 +128,7 @@ CASES = [  # B, Nq, Nk, Hq, Hk, D, mask, cap, bias, layout
     # capped scores over many keys
     (1, 530, 530, 4, 2, 72, dict(causal=True, prefix=True), 15.0, True, "packed"),
     (1, 150, 700, 2, 1, 64, dict(causal=True, window=90), 30.0, False, "bnhd"),
+    (1, 150, 600, 2, 1, 64, dict(causal=True), 256.0, False, "bnhd"),
     # few workgroups and long walks: keys and rows are dealt out in the backward
     (1, 911, 911, 2, 2, 96, dict(causal=True), 30.0, True, "packed"),
     (2, 801, 1001, 3, 1, 64, dict(causal=True, docs=3, pad=True), 0, False, "bhnd"),

@@ -79,7 +79,9 @@ def test_attention_refusals(L):
     for kw in (dict(B=-1), dict(Nq=-1), dict(Nk=-1), dict(Hk=0), dict(Hq=3), dict(D=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")), dict(scale=float("nan")), dict(cap=-1.0),
                dict(cap=float("nan")), dict(cap=float("inf"))):
         assert attend(L, shape(**kw)) == bad and attend_bwd(L, shape(**kw)) == bad, kw
-    for kw in (dict(D=60), dict(D=136), dict(D=256)):
+    for kw in (dict(scale=1e38), dict(scale=1e30, cap=1e-10)):
+        assert attend(L, shape(**kw)) == bad and attend_bwd(L, shape(**kw)) == bad, kw
+    for kw in (dict(D=60), dict(D=136), dict(D=256), dict(cap=257.0)):
         assert attend(L, shape(**kw)) == no and attend_bwd(L, shape(**kw)) == no, kw
         assert m.attention_bwd_q_workspace_bytes(shape(**kw)) == 0
     for kw in (dict(Nq=1 << 29, D=128), dict(Nk=1 << 28, D=64), dict(Nq=1 << 28, Hq=32), dict(B=1 << 24), dict(B=1 << 29, Hq=1 << 29, Hk=1 << 29)):
