@@ -756,9 +756,10 @@ template <typename T, int DP, bool CAP, bool BIAS, bool FINE> __device__ __force
     ab_put<T, DP>(mid, dv, undo_v, lane, s.D, [&](int i) __attribute__((always_inline)) { return j0 + i < s.Nk ? pv + int64_t(i) * a.dv.token : nullptr; });
 }
 
-// Both walks in one launch: the rows' workgroups fill in where the keys' run out (8 x 12 heads of 197 keys 23.6 -> 15.1 us, 32 x 12 46.2 ->
-// 44.1).  With many workgroups there is nothing to fill in, and dq alone has more waves (4 x 4 heads of 4001 keys: 390 us in two launches,
-// 402 in one).  Tiles of 64 keys for dq here, whose waves are few and wait for them (2 x 12 heads of 4096 keys 405 -> 395 us; 8 x 12 of 197 15.0 -> 15.4).
+// Both walks in one launch: the rows' workgroups fill in where the keys' run out (8 x 12 heads of 197 keys 23.6 -> 15.1 us, 2 x 4 heads of 4001
+// keys in documents 327 -> 225, 4 x 4 of 4096 543 -> 517).  With more workgroups there is less to fill in, and dq alone has more waves (4 x 4 heads of
+// 4001 keys, at the border: 390 us in two launches, 400 in one).  Tiles of 64 keys for dq here, whose waves are few and wait for them (2 x 12 heads of
+// 4096 keys 405 -> 395 us; 8 x 12 of 197 15.0 -> 15.4).
 template <typename T, int DP, bool CAP, bool BIAS, bool FINE>
 __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void k_attn_both(const AtBwd a)
 {
@@ -849,9 +850,11 @@ static AtBwdPlan at_bwd_plan(const mesa_attention &a, const bool codes[3])
     p.blocks = uint32_t(ceil_div(o.tiles, 4));
     p.key_blocks = uint32_t(ceil_div(a.Nk, kAbKeys));
     p.row_blocks = uint32_t(ceil_div(R, 128));
-    // few keys and long walks: the rows' tiles are dealt out to several workgroups and their sums added up
+    // Few keys and long walks: the rows' tiles are dealt out to several workgroups and their sums added up, so that there is a round of 512 (heads of 128,
+    // 4 x 4 of 4096 keys: one split 1038 us, two 1080; 3 x 4: two 817, one 889); two rounds where up to 64 elements one is full, as walks
+    // differ in length (4 x 4 heads of 4001 keys in documents 446 -> 432 us).
     const int64_t have = heads * p.key_blocks, most = o.tiles / 16;
-    int64_t n = have > 0 ? 1024 / have : 1, m = 1;
+    int64_t n = have > 0 ? (a.D <= 64 && have >= 512 ? 1024 / have : ceil_div(512, have)) : 1, m = 1;
     n = n > most ? most : n;
     // So few workgroups of either walk that compute units have nothing to do, and walks long enough to pay for the addition's launch (4 us): both
     // are dealt out, down to four tiles of rows or 192 keys each.  Two heads of 64, causal: 911 keys 32 -> 23 us, 2000 60 -> 33, 4000 111 -> 46;
@@ -881,7 +884,7 @@ static AtBwdPlan at_bwd_plan(const mesa_attention &a, const bool codes[3])
 template <typename T, int DP, bool CAP, bool BIAS, bool FINE> static mesa_status at_bwd_launch(const AtBwd &a, hipStream_t s)
 {
     const uint32_t keys = a.heads * a.key_blocks * a.splits, rows = a.heads * a.row_blocks * a.row_splits;
-    const bool both = DP == 64 ? keys < 1024 : keys + rows <= 256;      // two rounds of workgroups; one to a compute unit
+    const bool both = DP == 64 ? keys <= 1024 : keys + rows <= 256;      // two rounds of workgroups; one to a compute unit
     if (both) hipLaunchKernelGGL((k_attn_both<T, DP, CAP, BIAS, FINE>), dim3(keys + rows), dim3(256), 0, s, a);
     else hipLaunchKernelGGL((k_attn_dkv<T, DP, CAP, BIAS, FINE>), dim3(keys), dim3(256), 0, s, a);
     if (const mesa_status st = launch_status()) return st;
