@@ -11,8 +11,8 @@
 // binary16 storage: p goes into its products 2^8-fold, and ds with a power of two from the norms of do and v that keeps it
 // below 2^15 and as far as it can from the subnormal values, where products of long rows' probabilities and of small
 // gradients would lose their bits.  bfloat16 has the exponents of binary32 and needs neither.
-// Measured, 4 x 4096 x 16 heads of 128 on 4, causal, bfloat16: rows 29 us (145 MB, 5 TB/s), dk and dv 595 (four products, 0.92 PFLOP/s), their sums over
-// splits 28, dq 410 (three products, 1.0 PFLOP/s; a large library product 1.2).  32 x 12 heads of 197 keys, all codes: 13.5 and 43, by latency.
+// Measured, 4 x 4096 x 16 heads of 128 on 4, causal, bfloat16: rows 29 us (145 MB, 5 TB/s), dk and dv 600 (four products, 0.92 PFLOP/s),
+// dq 405 (three products, 1.0 PFLOP/s; a large library product 1.2).  32 x 12 heads of 197 keys, all codes: 13.5 and 43, by latency.
 #include "attention.hpp"
 
 namespace mesa {
